@@ -332,6 +332,116 @@ kvr_status kvr_select_to_boundary(int32_t n, int32_t edit_start, int32_t edit_en
 kvr_status kvr_transplant(kvr_ctx *ctx, const void *d_src, int32_t src_n_cap, void *d_dst, int32_t dst_n_cap,
                           const int32_t *h_positions, int32_t n_positions, void *stream);
 
+/* ---- Packed caches: a document's cache in codes of 4 or 8 bits
+ *
+ * A packed cache holds the rows of a cache (a row: one position's keys or values
+ * of one layer and kv head) in codes of `bits` = 4 or 8 bits.  Each 64 dimensions
+ * of a row (head_dim below or above a multiple of 64: the rest) share an offset m
+ * and a scale s, both bf16, and a code c in [0, 2^bits - 1]; the row's value is
+ * m + s * c.  A row's codes depend on that row alone, so any set of positions can
+ * be rewritten in place.  Packing a group of values x:
+ *   m = min x, rounded down to bf16
+ *   s = fl(fl(max x - m) * fl(1 / (2^bits - 1))), rounded up to bf16 (at least
+ *       2^-126; 0 when max x = m)
+ *   c = rint(fl(fl(x - m) * fl(1 / s))), ties to even; 0 when s = 0
+ * (fl: one fp32 operation), so an element is off by about s / 2 at most.  A group
+ * that holds a value that is not finite, or whose range overflows fp32, stands
+ * for NaN in all its elements.  The rows of other positions are never touched.
+ *
+ * Layout [n_layers][2][n_kv_heads][ceil(n_cap / 32)] blocks of 32 positions.  With
+ * W = 64 for head_dim <= 64 and 128 otherwise (the codes of dimensions from head_dim
+ * on are 0), a block is 4 * W * bits bytes of codes, then 32 * (W / 64) 32-bit words
+ * [position][group] with s in the low half and m in the high half.  Codes of
+ * position r (0 .. 31 within the block) and dimension d, all divisions integer:
+ *   keys, word q = ((r/16 * 4 + d/8 % 4) * 16 + r%16) * (W/32) + d/32:
+ *     4 bits: nibble (d%2) * 4 + d%8/2 of 32-bit word q
+ *     8 bits: byte d%8 of 64-bit word q
+ *   values, lane l = (r/4 % 4) * 16 + d%16:
+ *     4 bits: byte ((l * (W/32) + d/32) * 2 + r/16) * 4 + r%4, low nibble for
+ *             d/16 even, high nibble for d/16 odd
+ *     8 bits: byte ((l * (W/16) + d/16) * 2 + r/16) * 4 + r%4
+ * (the order in which the matrix units take them; nibbles and bytes count from the
+ * low end).  A packed cache is 16-byte aligned; kvr_packed_bytes() gives its size.
+ * It needs no initialisation: what no call wrote is not read, except by a query row
+ * whose position is behind it.
+ *
+ * In the calls below `bits` other than 4 or 8 is KVR_E_UNSUPPORTED. */
+
+/* Bytes of one document's packed cache, 0 for invalid arguments. */
+size_t kvr_packed_bytes(const kvr_dims *dims, int32_t n_cap, int32_t bits);
+
+/* One document of kvr_pack or kvr_unpack: positions h_positions (host, strictly
+ * ascending, copied during the call; NULL: all of [0, n_positions)) of a cache with
+ * n_cap slots and of a packed cache with packed_n_cap slots. */
+typedef struct {
+    void *d_cache;
+    int32_t n_cap;
+    void *d_packed;
+    int32_t packed_n_cap;
+    const int32_t *h_positions;
+    int32_t n_positions;
+} kvr_pack_doc;
+
+/* Quantise the listed positions of each document's cache, every layer and kv head,
+ * into its packed cache (a context goes to rest; after a repair of the cache, the
+ * repaired positions).  d_cache is only read.  The packed caches of one call must
+ * not overlap, nor overlap a cache that is read.  Errors: KVR_E_ARG (NULL context,
+ * caches, bad position lists, misaligned or overlapping caches), KVR_E_RANGE (a
+ * position outside [0, min(n_cap, packed_n_cap))), KVR_E_UNSUPPORTED, KVR_E_NOMEM,
+ * KVR_E_HIP. */
+kvr_status kvr_pack(kvr_ctx *ctx, const kvr_pack_doc *docs, int32_t n_docs, int32_t bits, void *stream);
+
+/* The reverse: write the values m + s * c of the listed positions, rounded to the
+ * context's dtype, into d_cache; d_packed is only read and other slots of d_cache are
+ * not touched.  Errors as kvr_pack. */
+kvr_status kvr_unpack(kvr_ctx *ctx, const kvr_pack_doc *docs, int32_t n_docs, int32_t bits, void *stream);
+
+/* Rows of one document in a call over packed caches.  The rows of a call's documents
+ * follow each other in its row arrays, in the documents' order. */
+typedef struct {
+    void *d_packed;             /* packed cache of n_cap slots */
+    int32_t n_cap;              /* 1 <= n_cap <= max_ctx */
+    const int32_t *h_positions; /* the rows' positions (host, copied during the call) */
+    int32_t n_rows;
+} kvr_packed_rows;
+
+/* Quantise fresh key and value rows of one layer into packed caches.  d_k and d_v
+ * (device, the context's dtype, aligned to it; keys after the rotary embedding) hold
+ * a row of n_kv_heads * head_dim values per listed position, row_stride values
+ * apart.  A document's positions are strictly ascending in [0, n_cap); no two
+ * documents with rows share cache memory.  Errors: KVR_E_ARG (NULL pointers,
+ * unsorted positions, misaligned or overlapping caches), KVR_E_RANGE (layer, n_cap,
+ * a position, or row_stride < n_kv_heads * head_dim), KVR_E_UNSUPPORTED,
+ * KVR_E_NOMEM, KVR_E_HIP. */
+kvr_status kvr_append_packed(kvr_ctx *ctx, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                             const void *d_k, const void *d_v, int64_t row_stride, void *stream);
+
+/* Causal grouped-query attention of query rows over one layer of packed caches, scale
+ * 1/sqrt(head_dim): a row at position p attends over slots 0 .. p of its document,
+ * whatever the other slots hold.  Positions are in [-1, n_cap), in any order, and may
+ * repeat; a row at -1 (an idle slot of a batch) sees nothing and its output is zero.
+ * Documents may share a packed cache, which is only read.  d_q and d_out (device, the
+ * context's dtype, aligned to it, not overlapping) hold a row of n_heads * head_dim
+ * values per listed row, q_stride and out_stride values apart (queries after the
+ * rotary embedding).  Scores, softmax and sums are fp32; the products take the codes,
+ * not rounded values.  Errors: KVR_E_ARG (NULL or misaligned pointers), KVR_E_RANGE
+ * (layer, n_cap, a position, a stride below n_heads * head_dim, or more than
+ * 2^31 - 1 rows times heads), KVR_E_UNSUPPORTED, KVR_E_NOMEM, KVR_E_HIP. */
+kvr_status kvr_attention_packed(kvr_ctx *ctx, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                                const void *d_q, int64_t q_stride, void *d_out, int64_t out_stride, void *stream);
+
+/* kvr_prefill, kvr_repair, kvr_score and kvr_generate over packed caches of n_cap
+ * slots: fresh keys and values are quantised as they are written, before any row of
+ * the layer attends, and attention reads the packed cache (in kvr_doc, d_cache is the
+ * packed cache).  Arguments, semantics and errors are those calls'. */
+kvr_status kvr_prefill_packed(kvr_ctx *ctx, const int32_t *d_tokens, int32_t n, int32_t n_cap, void *d_packed,
+                              int32_t bits, float *d_hidden_out, void *stream);
+kvr_status kvr_repair_packed(kvr_ctx *ctx, const kvr_doc *docs, int32_t n_docs, int32_t bits, void *stream);
+kvr_status kvr_score_packed(kvr_ctx *ctx, void *d_packed, int32_t bits, int32_t n, int32_t n_cap,
+                            const int32_t *d_tokens, int32_t m, float *d_logprob, int32_t *d_argmax, void *stream);
+kvr_status kvr_generate_packed(kvr_ctx *ctx, void *d_packed, int32_t bits, int32_t n, int32_t n_cap, int32_t *d_tokens,
+                               int32_t q, int32_t max_new, void *stream);
+
 /* Per-step GPU time accounting, a tracing aid for benchmarks.  While enabled
  * (it is off after kvr_create), every kernel launch of a prefill or repair
  * pass is made with a pair of HIP events that the dispatch records at the

@@ -25,6 +25,8 @@ STATUS_NAMES = {0: "KVR_OK", 1: "KVR_E_ARG", 2: "KVR_E_RANGE", 3: "KVR_E_UNSUPPO
 EXPORTED = ("kvr_create", "kvr_destroy", "kvr_cache_bytes", "kvr_workspace_bytes", "kvr_prefill", "kvr_repair",
             "kvr_select", "kvr_select_to_boundary", "kvr_transplant", "kvr_score", "kvr_generate", "kvr_select_cacheblend",
             "kvr_select_attention", "kvr_select_attention_noalloc", "kvr_answer_logprob", "kvr_margin_recovery", "kvr_flipped",
+            "kvr_packed_bytes", "kvr_pack", "kvr_unpack", "kvr_append_packed", "kvr_attention_packed", "kvr_prefill_packed",
+            "kvr_repair_packed", "kvr_score_packed", "kvr_generate_packed",
             "kvr_profile_enable", "kvr_profile_read", "kvr_last_error")
 
 
@@ -55,6 +57,15 @@ class kvr_doc(ctypes.Structure):
     _fields_ = [("d_cache", c_void_p), ("n", c_int32), ("n_cap", c_int32), ("d_tokens_new", c_void_p),
                 ("edit_start", c_int32), ("edit_end", c_int32), ("h_positions", POINTER(c_int32)),
                 ("n_positions", c_int32), ("d_hidden_out", c_void_p)]
+
+
+class kvr_pack_doc(ctypes.Structure):
+    _fields_ = [("d_cache", c_void_p), ("n_cap", c_int32), ("d_packed", c_void_p), ("packed_n_cap", c_int32),
+                ("h_positions", POINTER(c_int32)), ("n_positions", c_int32)]
+
+
+class kvr_packed_rows(ctypes.Structure):
+    _fields_ = [("d_packed", c_void_p), ("n_cap", c_int32), ("h_positions", POINTER(c_int32)), ("n_rows", c_int32)]
 
 
 _lib = None
@@ -111,6 +122,27 @@ def load() -> ctypes.CDLL:
     lib.kvr_flipped.argtypes = [POINTER(c_int32), c_int32, POINTER(c_int32), c_int32, POINTER(c_int32), c_int32,
                                 POINTER(c_int32)]
     lib.kvr_flipped.restype = c_int
+    lib.kvr_packed_bytes.argtypes = [POINTER(kvr_dims), c_int32, c_int32]
+    lib.kvr_packed_bytes.restype = c_size_t
+    for name in ("kvr_pack", "kvr_unpack"):
+        fn = getattr(lib, name)
+        fn.argtypes = [c_void_p, POINTER(kvr_pack_doc), c_int32, c_int32, c_void_p]
+        fn.restype = c_int
+    lib.kvr_append_packed.argtypes = [c_void_p, c_int32, c_int32, POINTER(kvr_packed_rows), c_int32, c_void_p, c_void_p,
+                                      c_int64, c_void_p]
+    lib.kvr_append_packed.restype = c_int
+    lib.kvr_attention_packed.argtypes = [c_void_p, c_int32, c_int32, POINTER(kvr_packed_rows), c_int32, c_void_p, c_int64,
+                                         c_void_p, c_int64, c_void_p]
+    lib.kvr_attention_packed.restype = c_int
+    lib.kvr_prefill_packed.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p]
+    lib.kvr_prefill_packed.restype = c_int
+    lib.kvr_repair_packed.argtypes = [c_void_p, POINTER(kvr_doc), c_int32, c_int32, c_void_p]
+    lib.kvr_repair_packed.restype = c_int
+    lib.kvr_score_packed.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                     c_void_p]
+    lib.kvr_score_packed.restype = c_int
+    lib.kvr_generate_packed.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32, c_int32, c_void_p]
+    lib.kvr_generate_packed.restype = c_int
     lib.kvr_profile_enable.argtypes = [c_void_p, c_int32]
     lib.kvr_profile_enable.restype = c_int
     lib.kvr_profile_read.argtypes = [c_void_p, c_int32, POINTER(c_char_p), POINTER(c_double), POINTER(c_int64),
@@ -271,3 +303,84 @@ def kvr_flipped(continuation: Sequence[int], a_new: Sequence[int], a_old: Sequen
     _check(load().kvr_flipped(arrs[0], len(continuation), arrs[1], len(a_new), arrs[2], len(a_old),
                               ctypes.byref(out)))
     return bool(out.value)
+
+
+def kvr_packed_bytes(dims: kvr_dims, n_cap: int, bits: int) -> int:
+    return load().kvr_packed_bytes(ctypes.byref(dims), n_cap, bits)
+
+
+def _positions(positions: Sequence[int]):
+    return (c_int32 * max(1, len(positions)))(*positions)
+
+
+def make_pack_docs(docs: Sequence[tuple]):
+    """The document list of kvr_pack and kvr_unpack, from tuples (d_cache, n_cap,
+    d_packed, packed_n_cap, positions) with positions a list, or a count n for
+    [0, n).  The arrays are kept alive on the returned object, which can be used for
+    several calls."""
+    arr, keep = (kvr_pack_doc * max(1, len(docs)))(), []
+    for d, (cache, n_cap, packed, packed_n_cap, positions) in zip(arr, docs):
+        d.d_cache, d.n_cap, d.d_packed, d.packed_n_cap = cache, n_cap, packed, packed_n_cap
+        if isinstance(positions, int):
+            d.n_positions = positions
+        else:
+            keep.append(_positions(positions))
+            d.h_positions, d.n_positions = ctypes.cast(keep[-1], POINTER(c_int32)), len(positions)
+    arr._keep, arr._count = keep, len(docs)
+    return arr
+
+
+def make_packed_rows(docs: Sequence[tuple]):
+    """The document list of kvr_append_packed and kvr_attention_packed, from tuples
+    (d_packed, n_cap, positions).  As make_pack_docs; a list's positions can be changed
+    between calls through its elements' h_positions."""
+    arr, keep = (kvr_packed_rows * max(1, len(docs)))(), []
+    for d, (packed, n_cap, positions) in zip(arr, docs):
+        keep.append(_positions(positions))
+        d.d_packed, d.n_cap = packed, n_cap
+        d.h_positions, d.n_rows = ctypes.cast(keep[-1], POINTER(c_int32)), len(positions)
+    arr._keep, arr._count = keep, len(docs)
+    return arr
+
+
+def kvr_pack(ctx: int, docs, bits: int, stream: Optional[int] = None) -> None:
+    """docs: from make_pack_docs."""
+    _check(load().kvr_pack(ctx, docs, docs._count, bits, stream), ctx)
+
+
+def kvr_unpack(ctx: int, docs, bits: int, stream: Optional[int] = None) -> None:
+    """docs: from make_pack_docs."""
+    _check(load().kvr_unpack(ctx, docs, docs._count, bits, stream), ctx)
+
+
+def kvr_append_packed(ctx: int, layer: int, bits: int, docs, d_k: Optional[int], d_v: Optional[int], row_stride: int,
+                      stream: Optional[int] = None) -> None:
+    """docs: from make_packed_rows."""
+    _check(load().kvr_append_packed(ctx, layer, bits, docs, docs._count, d_k, d_v, row_stride, stream), ctx)
+
+
+def kvr_attention_packed(ctx: int, layer: int, bits: int, docs, d_q: Optional[int], q_stride: int, d_out: Optional[int],
+                         out_stride: int, stream: Optional[int] = None) -> None:
+    """docs: from make_packed_rows."""
+    _check(load().kvr_attention_packed(ctx, layer, bits, docs, docs._count, d_q, q_stride, d_out, out_stride, stream), ctx)
+
+
+def kvr_prefill_packed(ctx: int, d_tokens: int, n: int, n_cap: int, d_packed: int, bits: int,
+                       d_hidden_out: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(load().kvr_prefill_packed(ctx, d_tokens, n, n_cap, d_packed, bits, d_hidden_out, stream), ctx)
+
+
+def kvr_repair_packed(ctx: int, docs: Sequence[kvr_doc], bits: int, stream: Optional[int] = None) -> None:
+    """docs: from make_doc, with the packed cache as d_cache."""
+    arr = (kvr_doc * max(1, len(docs)))(*docs)
+    _check(load().kvr_repair_packed(ctx, arr, len(docs), bits, stream), ctx)
+
+
+def kvr_score_packed(ctx: int, d_packed: int, bits: int, n: int, n_cap: int, d_tokens: int, m: int,
+                     d_logprob: Optional[int], d_argmax: Optional[int] = None, stream: Optional[int] = None) -> None:
+    _check(load().kvr_score_packed(ctx, d_packed, bits, n, n_cap, d_tokens, m, d_logprob, d_argmax, stream), ctx)
+
+
+def kvr_generate_packed(ctx: int, d_packed: int, bits: int, n: int, n_cap: int, d_tokens: int, q: int, max_new: int,
+                        stream: Optional[int] = None) -> None:
+    _check(load().kvr_generate_packed(ctx, d_packed, bits, n, n_cap, d_tokens, q, max_new, stream), ctx)

@@ -20,6 +20,7 @@
 
 #include "../../include/kvr.h"
 #include "common.h"
+#include "packed.h"
 
 using namespace kvr;
 
@@ -42,9 +43,18 @@ struct Tables {
     std::vector<AttnItem> items;
     std::vector<CombineItem> comb;
     std::vector<Block> blocks;
+    // packed caches: the launches of one layer's attention
+    struct PackedLaunch {
+        PackedTable table;
+        int n_docs, n_items, n_cg;
+        bool combine;
+    };
+    std::vector<PackedLaunch> packed;
+    PackedShape packed_shape{1, 1};
+    int packed_range = 0;
     int att_mt = 1;  // 16-row tiles per attention item (rows of a row block / 16)
     void clear() {
-        rows.clear(); docs.clear(); items.clear(); comb.clear(); blocks.clear();
+        rows.clear(); docs.clear(); items.clear(); comb.clear(); blocks.clear(); packed.clear();
         att_mt = 1;
     }
 };
@@ -498,20 +508,184 @@ struct MassHook {
     float *part;  // [Hkv][n]
 };
 
+// ---- packed caches
+
+size_t packed_bytes(const kvr_dims &d, int32_t n_cap, int bits) {
+    return (size_t)d.n_layers * 2 * d.n_kv_heads * pk_blocks(n_cap) * pk_block_bytes(pk_width(d.head_dim), bits);
+}
+
+// Fills one launch's table.
+struct TableFill {
+    PackedTable *t;
+    int docs = 0, tail = PK_WORDS;
+    explicit TableFill(PackedTable *table) : t(table) {}
+    uint32_t *entry(int i) { return t->w + i * PK_ENTRY; }
+    // An entry for the first rows of a list of n positions (`step` words apart):
+    // returns how many, 0 when the table is full.  A run of consecutive positions
+    // needs no list; one of an entry's length or more gets an entry of its own if
+    // `runs`, and the whole list is one entry that reads the pass's row table if
+    // `row_table`.
+    int add(const void *packed, int blocks, int row0, const int32_t *pos, int step, int n, bool runs, bool row_table) {
+        const int room = tail - (docs + 1) * PK_ENTRY;
+        if (room < 0) return 0;
+        auto run = [&](int i) {  // length of the run that starts at i
+            int j = i + 1;
+            while (j < n && pos[(size_t)j * step] - pos[(size_t)i * step] == j - i) ++j;
+            return j - i;
+        };
+        int k = run(0);
+        uint32_t ref = PK_RUN;
+        if (k < n && !(runs && k >= PK_ENTRY)) {
+            if (row_table) {
+                ref = PK_ROWS;
+                k = n;
+            } else {
+                int last = k;
+                while (last < n && last < room) {
+                    const int more = run(last);
+                    if (runs && more >= PK_ENTRY) break;
+                    last += more;
+                }
+                k = std::min(std::min(last, n), room);
+                if (k < 1) return 0;
+                tail -= k;
+                ref = (uint32_t)tail;
+                for (int i = 0; i < k; ++i) t->w[tail + i] = (uint32_t)pos[(size_t)i * step];
+            }
+        }
+        uint32_t *e = entry(docs++);
+        e[PKE_PACKED] = (uint32_t)(uintptr_t)packed;
+        e[PKE_PACKED + 1] = (uint32_t)((uintptr_t)packed >> 32);
+        e[PKE_BLOCKS] = (uint32_t)blocks;
+        e[PKE_ROW0] = (uint32_t)row0;
+        e[PKE_ROWS] = (uint32_t)k;
+        e[PKE_REF] = ref;
+        e[PKE_POS] = (uint32_t)pos[0];
+        return k;
+    }
+};
+
+// The query rows of one document: positions `step` words apart.
+struct PackedQuery {
+    const void *packed;
+    int n_cap, row0, n;
+    const int32_t *pos;
+    int step;
+};
+
+// The attention launches of rows over packed caches (t.packed): which columns a
+// block takes, and into how many key ranges a document's keys are cut.
+template <typename DocAt>
+void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_table) {
+    const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
+    t.packed.clear();
+    int most = 0;
+    for (int i = 0; i < n_docs; ++i) most = std::max(most, doc(i).n);
+    const long long most_cols = (long long)most * G;
+    const PackedShape sh = {1, most_cols <= 16 ? 1 : most_cols <= 32 ? 2 : 4};
+    const int cols = pk_cols(sh), kw = PK_ATT_WAVES / sh.cw;
+    long long items = 0, units = 0;
+    int longest = 0;
+    for (int i = 0; i < n_docs; ++i) {
+        const PackedQuery q = doc(i);
+        int keys = 0;
+        for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
+        const long long ncg = ((long long)q.n * G + cols - 1) / cols;
+        items += ncg * Hkv;
+        units += ncg * Hkv * pk_blocks(keys);
+        longest = std::max(longest, keys);
+    }
+    // About three blocks to a compute unit; every wavefront has at least two of
+    // the 32-key steps.
+    long long range = pk_blocks(std::max(longest, 1));
+    if (items < 768) range = std::min(range, std::max<long long>(2 * kw, (units + 767) / 768));
+    const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
+    const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
+    while (range < pk_blocks(longest) && (pk_blocks(longest) + range - 1) / range * per_row > slots) range *= 2;
+    t.packed_shape = sh;
+    t.packed_range = (int)range * PK_BLOCK;
+
+    std::vector<Tables::PackedLaunch> &out = t.packed;
+    TableFill fill(nullptr);
+    int used = 0;  // partial slots of the launch
+    auto open = [&] {
+        out.emplace_back();
+        Tables::PackedLaunch &l = out.back();
+        l.n_docs = l.n_items = l.n_cg = 0;
+        l.combine = false;
+        fill = TableFill(&l.table);
+        used = 0;
+    };
+    for (int i = 0; i < n_docs; ++i) {
+        PackedQuery q = doc(i);
+        while (q.n > 0) {
+            if (out.empty()) open();
+            int keys = 0;
+            for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
+            const int ns = std::max(1, (int)((pk_blocks(keys) + range - 1) / range));
+            long long fit = q.n;
+            if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);
+            const int before = fill.docs;
+            const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, false, row_table);
+            if (n == 0) {
+                open();
+                continue;
+            }
+            Tables::PackedLaunch &l = out.back();
+            uint32_t *e = fill.entry(before);
+            const int ncg = (int)(((long long)n * G + cols - 1) / cols);
+            e[PKE_ITEM0] = (uint32_t)l.n_items;
+            e[PKE_CG0] = (uint32_t)l.n_cg;
+            e[PKE_SPLITS] = (uint32_t)ns;
+            e[PKE_PART0] = (uint32_t)used;
+            e[PKE_KEYS] = (uint32_t)keys;
+            l.n_docs = fill.docs;
+            l.n_items += ncg * ns;
+            l.n_cg += ncg;
+            if (ns > 1) {
+                l.combine = true;
+                used += ncg * ns;
+            }
+            q.row0 += n;
+            q.pos += (size_t)n * q.step;
+            q.n -= n;
+        }
+    }
+}
+
+// The kernel arguments of one of plan_packed's launches; `a` describes the rows.
+PackedAttnArgs packed_args(const kvr_ctx *c, const Tables &t, const Tables::PackedLaunch &l, PackedAttnArgs a) {
+    a.Hq = c->d.n_heads;
+    a.Hkv = c->d.n_kv_heads;
+    a.hd = c->d.head_dim;
+    a.part = c->attn_part;
+    a.n_docs = l.n_docs;
+    a.n_items = l.n_items;
+    a.n_cg = l.n_cg;
+    a.range = t.packed_range;
+    return a;
+}
+
 // Upload the tables of a pass and enqueue its kernels.  kv_layer >= 0 stops
 // the pass at that layer once its fresh keys/values are in the cache (layers
 // below it run in full; no final norm).  lm_operand: the final norm's rows go
 // to Xn as the LM head's operand (packed head: operand order) instead of to
-// the documents' hidden rows.
+// the documents' hidden rows.  bits != 0: the documents' caches are packed.
 kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, const MassHook *mh = nullptr,
-                    bool lm_operand = false) {
+                    bool lm_operand = false, int bits = 0) {
     const kvr_dims &d = c->d;
     const int R = (int)t.rows.size();
     if (R == 0) return KVR_OK;
     const bool attn_mfma = !c->force_simple && attention_mfma_ok(c->bf16, d.n_heads, d.n_kv_heads, d.head_dim);
     const bool sk = skinny_pass_ok(c, R);
     const bool op = c->wpk != nullptr;  // matrix operands in MFMA operand order (both packed-weight kernels)
-    plan_attention(c, t, attn_mfma);
+    if (bits)
+        plan_packed(c, t, (int)t.docs.size(), [&](int i) {
+            const DocInfo &dc = t.docs[i];
+            return PackedQuery{dc.cache, dc.n_cap, dc.row0, dc.nrows, &t.rows[dc.row0].pos, (int)(sizeof(RowInfo) / 4)};
+        }, true);
+    else
+        plan_attention(c, t, attn_mfma);
     if ((int)t.items.size() > c->items_cap || (int)t.comb.size() > c->comb_cap)
         return fail(c, KVR_E_RANGE, "attention plan exceeds the context's item capacity");
 
@@ -649,11 +823,28 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
             KVR_CHECK(linear(c, EPI_STORE, qa, s), "qkv", ST_QKV);
             qkv_split = qa.split;
         }
-        KVR_CHECK(launch_rope_scatter(bf, c->P, qkv_split, w.bq, w.bk, w.bv, rows, docs, R, l, d.n_heads, d.n_kv_heads,
-                                      hd, c->rope_cos, c->rope_sin, c->Qb, c->Qb_lo, s), "rope_scatter", ST_ROPE);
+        if (bits)
+            KVR_CHECK(launch_rope_pack(bf, bits, c->P, qkv_split, w.bq, w.bk, w.bv, rows, docs, R, l, d.n_heads,
+                                       d.n_kv_heads, hd, c->rope_cos, c->rope_sin, c->Qb, c->Qb_lo, s), "rope_pack", ST_ROPE);
+        else
+            KVR_CHECK(launch_rope_scatter(bf, c->P, qkv_split, w.bq, w.bk, w.bv, rows, docs, R, l, d.n_heads, d.n_kv_heads,
+                                          hd, c->rope_cos, c->rope_sin, c->Qb, c->Qb_lo, s), "rope_scatter", ST_ROPE);
         if (l == kv_layer) return KVR_OK;
         float *lse = mh ? mh->lse : nullptr;
-        if (attn_mfma)
+        PackedAttnArgs pa{};
+        pa.q = c->Qb; pa.q_lo = c->Qb_lo; pa.q_stride = qd;
+        pa.out = c->Ob; pa.out_lo = c->Ob_lo; pa.out_stride = qd; pa.o_perm = op;
+        pa.rows = rows; pa.layer = l;
+        for (const auto &pl : t.packed) {  // packed caches only
+            KVR_CHECK(launch_attention_packed(bf, bits, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
+                      "attention_packed", ST_ATTN);
+            if (pl.combine)
+                KVR_CHECK(launch_attention_packed_combine(bf, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
+                          "attention_packed_combine", ST_COMBINE);
+        }
+        if (bits) {
+            // done above
+        } else if (attn_mfma)
             KVR_CHECK(launch_attention_mfma((const bf16_t *)c->Qb, (const bf16_t *)c->Qb_lo, rows, items,
                                             (int)t.items.size(), t.att_mt, l, d.n_heads, d.n_kv_heads, hd, c->attn_part,
                                             (bf16_t *)c->Ob, (bf16_t *)c->Ob_lo, op, lse, s),
@@ -747,7 +938,7 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
 // log-softmax in blocks of SCORE_ROWS rows: lp[j] = log p(tokens[n+j+1]) for
 // j < m-1, argmax[j] for j < m, and *next = argmax of row m-1.
 kvr_status score_block(kvr_ctx *c, void *cache, int n, int n_cap, const int32_t *tokens, int m, float *lp,
-                       int32_t *argmax, int32_t *next, hipStream_t s) {
+                       int32_t *argmax, int32_t *next, int bits, hipStream_t s) {
     const kvr_dims &d = c->d;
     const int D = d.d_model, V = d.vocab;
     Tables &t = c->tab;
@@ -755,7 +946,7 @@ kvr_status score_block(kvr_ctx *c, void *cache, int n, int n_cap, const int32_t 
     t.docs.push_back(DocInfo{cache, tokens, nullptr, n + m, n_cap, 0, m});
     t.rows.reserve(m);
     for (int j = 0; j < m; ++j) t.rows.push_back(RowInfo{n + j, 0, j, 0});
-    kvr_status st = run_pass(c, t, s, -1, nullptr, true);
+    kvr_status st = run_pass(c, t, s, -1, nullptr, true, bits);
     if (st != KVR_OK) return st;
     const SkinnyPlan plan = plan_skinny(V / 16, D, SCORE_ROWS, false, 16, "KVR_NT_LM", "KVR_SPLIT_LM");
 #define KVR_SCHECK(expr, what, step)                                                \
@@ -819,6 +1010,27 @@ kvr_status check_dims(const kvr_dims *d) {
     // and over the fused Q|K|V row of (n_heads + 2 n_kv_heads) head_dim values
     if (d->d_model % 4 != 0 || d->d_model > 16384 || ((d->n_heads + 2 * d->n_kv_heads) * d->head_dim) % 4 != 0)
         return KVR_E_UNSUPPORTED;
+    return KVR_OK;
+}
+
+// Runs the body of an entry point; what it throws (host memory) becomes a status.
+template <typename Body>
+kvr_status guarded(kvr_ctx *c, Body body) {
+    try {
+        return body();
+    } catch (...) {
+        if (c) c->err.clear();  // no memory for a message
+        return KVR_E_NOMEM;
+    }
+}
+
+// Positions of one document of a packed call, in [lo, hi); `sorted`: strictly ascending.
+template <typename Fail>
+kvr_status check_positions(Fail bad, const int32_t *pos, int32_t n, int32_t lo, int32_t hi, bool sorted) {
+    for (int i = 0; i < n; ++i) {
+        if (pos[i] < lo || pos[i] >= hi) return bad(KVR_E_RANGE, "position out of range");
+        if (sorted && i > 0 && pos[i] <= pos[i - 1]) return bad(KVR_E_ARG, "positions must be strictly ascending");
+    }
     return KVR_OK;
 }
 
@@ -1038,13 +1250,20 @@ void kvr_destroy(kvr_ctx *c) {
     delete c;
 }
 
-kvr_status kvr_prefill(kvr_ctx *c, const int32_t *d_tokens, int32_t n, int32_t n_cap, void *d_cache,
-                       float *d_hidden_out, void *stream) {
-    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_prefill: NULL context");
-    if (!d_tokens || !d_cache) return fail(c, KVR_E_ARG, "kvr_prefill: NULL tokens or cache");
-    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, "kvr_prefill: cache must be 16-byte aligned");
+// Bits of a packed cache's codes that a call names.
+static kvr_status check_bits(kvr_ctx *c, const char *who, int32_t bits) {
+    return bits == 4 || bits == 8 ? KVR_OK : fail(c, KVR_E_UNSUPPORTED, std::string(who) + ": packed caches hold 4 or 8 bits");
+}
+
+// Shared body of kvr_prefill (bits 0) and kvr_prefill_packed.
+static kvr_status prefill(kvr_ctx *c, const char *name, const int32_t *d_tokens, int32_t n, int32_t n_cap, void *d_cache,
+                          int32_t bits, float *d_hidden_out, void *stream) {
+    const std::string who = name;
+    if (!c) return fail(nullptr, KVR_E_ARG, who + ": NULL context");
+    if (!d_tokens || !d_cache) return fail(c, KVR_E_ARG, who + ": NULL tokens or cache");
+    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, who + ": cache must be 16-byte aligned");
     if (n < 1 || n > n_cap || n_cap > c->d.max_ctx)
-        return fail(c, KVR_E_RANGE, "kvr_prefill: need 1 <= n <= n_cap <= max_ctx");
+        return fail(c, KVR_E_RANGE, who + ": need 1 <= n <= n_cap <= max_ctx");
     DeviceGuard g(c->device);
     hipStream_t s = (hipStream_t)stream;
     const int chunk = c->rows_cap;
@@ -1055,10 +1274,15 @@ kvr_status kvr_prefill(kvr_ctx *c, const int32_t *d_tokens, int32_t n, int32_t n
         t.docs.push_back(DocInfo{d_cache, d_tokens, d_hidden_out, n, n_cap, 0, c1 - c0});
         t.rows.reserve(c1 - c0);
         for (int p = c0; p < c1; ++p) t.rows.push_back(RowInfo{p, 0, p, 0});
-        kvr_status st = run_pass(c, t, s);
+        kvr_status st = run_pass(c, t, s, -1, nullptr, false, bits);
         if (st != KVR_OK) return st;
     }
     return KVR_OK;
+}
+
+kvr_status kvr_prefill(kvr_ctx *c, const int32_t *d_tokens, int32_t n, int32_t n_cap, void *d_cache,
+                       float *d_hidden_out, void *stream) {
+    return prefill(c, "kvr_prefill", d_tokens, n, n_cap, d_cache, 0, d_hidden_out, stream);
 }
 
 kvr_status kvr_transplant(kvr_ctx *c, const void *d_src, int32_t src_n_cap, void *d_dst, int32_t dst_n_cap,
@@ -1113,39 +1337,53 @@ kvr_status kvr_transplant(kvr_ctx *c, const void *d_src, int32_t src_n_cap, void
     return KVR_OK;
 }
 
-kvr_status kvr_score(kvr_ctx *c, void *d_cache, int32_t n, int32_t n_cap, const int32_t *d_tokens, int32_t m,
-                     float *d_logprob, int32_t *d_argmax, void *stream) {
-    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_score: NULL context");
-    if (!d_cache || !d_tokens) return fail(c, KVR_E_ARG, "kvr_score: NULL cache or tokens");
-    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, "kvr_score: cache must be 16-byte aligned");
-    if (m > 1 && !d_logprob) return fail(c, KVR_E_ARG, "kvr_score: NULL log-probability output");
+// Shared body of kvr_score (bits 0) and kvr_score_packed.
+static kvr_status score(kvr_ctx *c, const char *name, void *d_cache, int32_t bits, int32_t n, int32_t n_cap,
+                        const int32_t *d_tokens, int32_t m, float *d_logprob, int32_t *d_argmax, void *stream) {
+    const std::string who = name;
+    if (!c) return fail(nullptr, KVR_E_ARG, who + ": NULL context");
+    if (!d_cache || !d_tokens) return fail(c, KVR_E_ARG, who + ": NULL cache or tokens");
+    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, who + ": cache must be 16-byte aligned");
+    if (m > 1 && !d_logprob) return fail(c, KVR_E_ARG, who + ": NULL log-probability output");
     if (n < 0 || m < 1 || (long long)n + m > n_cap || n_cap > c->d.max_ctx)
-        return fail(c, KVR_E_RANGE, "kvr_score: need n >= 0, m >= 1, n + m <= n_cap <= max_ctx");
-    if (m > c->rows_cap) return fail(c, KVR_E_RANGE, "kvr_score: more appended tokens than one pass holds");
+        return fail(c, KVR_E_RANGE, who + ": need n >= 0, m >= 1, n + m <= n_cap <= max_ctx");
+    if (m > c->rows_cap) return fail(c, KVR_E_RANGE, who + ": more appended tokens than one pass holds");
     DeviceGuard g(c->device);
     kvr_status st = score_buffers(c);
     if (st != KVR_OK) return st;
-    return score_block(c, d_cache, n, n_cap, d_tokens, m, d_logprob, d_argmax, nullptr, (hipStream_t)stream);
+    return score_block(c, d_cache, n, n_cap, d_tokens, m, d_logprob, d_argmax, nullptr, bits, (hipStream_t)stream);
 }
 
-kvr_status kvr_generate(kvr_ctx *c, void *d_cache, int32_t n, int32_t n_cap, int32_t *d_tokens, int32_t q,
-                        int32_t max_new, void *stream) {
-    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_generate: NULL context");
-    if (!d_cache || !d_tokens) return fail(c, KVR_E_ARG, "kvr_generate: NULL cache or tokens");
-    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, "kvr_generate: cache must be 16-byte aligned");
+kvr_status kvr_score(kvr_ctx *c, void *d_cache, int32_t n, int32_t n_cap, const int32_t *d_tokens, int32_t m,
+                     float *d_logprob, int32_t *d_argmax, void *stream) {
+    return score(c, "kvr_score", d_cache, 0, n, n_cap, d_tokens, m, d_logprob, d_argmax, stream);
+}
+
+// Shared body of kvr_generate (bits 0) and kvr_generate_packed.
+static kvr_status generate(kvr_ctx *c, const char *name, void *d_cache, int32_t bits, int32_t n, int32_t n_cap,
+                           int32_t *d_tokens, int32_t q, int32_t max_new, void *stream) {
+    const std::string who = name;
+    if (!c) return fail(nullptr, KVR_E_ARG, who + ": NULL context");
+    if (!d_cache || !d_tokens) return fail(c, KVR_E_ARG, who + ": NULL cache or tokens");
+    if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, who + ": cache must be 16-byte aligned");
     if (n < 0 || q < 1 || max_new < 1 || (long long)n + q + max_new - 1 > n_cap || n_cap > c->d.max_ctx)
-        return fail(c, KVR_E_RANGE, "kvr_generate: need n >= 0, q >= 1, max_new >= 1, n + q + max_new - 1 <= n_cap <= max_ctx");
-    if (q > c->rows_cap) return fail(c, KVR_E_RANGE, "kvr_generate: query longer than one pass holds");
+        return fail(c, KVR_E_RANGE, who + ": need n >= 0, q >= 1, max_new >= 1, n + q + max_new - 1 <= n_cap <= max_ctx");
+    if (q > c->rows_cap) return fail(c, KVR_E_RANGE, who + ": query longer than one pass holds");
     DeviceGuard g(c->device);
     kvr_status st = score_buffers(c);
     if (st != KVR_OK) return st;
     hipStream_t s = (hipStream_t)stream;
     // the query block, then one row per generated token; every next id is
     // written on the device and read back by the following pass
-    st = score_block(c, d_cache, n, n_cap, d_tokens, q, nullptr, nullptr, d_tokens + n + q, s);
+    st = score_block(c, d_cache, n, n_cap, d_tokens, q, nullptr, nullptr, d_tokens + n + q, bits, s);
     for (int i = 1; i < max_new && st == KVR_OK; ++i)
-        st = score_block(c, d_cache, n + q + i - 1, n_cap, d_tokens, 1, nullptr, nullptr, d_tokens + n + q + i, s);
+        st = score_block(c, d_cache, n + q + i - 1, n_cap, d_tokens, 1, nullptr, nullptr, d_tokens + n + q + i, bits, s);
     return st;
+}
+
+kvr_status kvr_generate(kvr_ctx *c, void *d_cache, int32_t n, int32_t n_cap, int32_t *d_tokens, int32_t q,
+                        int32_t max_new, void *stream) {
+    return generate(c, "kvr_generate", d_cache, 0, n, n_cap, d_tokens, q, max_new, stream);
 }
 
 // Grow the selectors' scratch to at least `need` bytes (waits for the stream
@@ -1321,13 +1559,15 @@ kvr_status kvr_profile_read(kvr_ctx *c, int32_t capacity, const char **names, do
     return KVR_OK;
 }
 
-kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *stream) {
-    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_repair: NULL context");
-    if (n_docs < 0 || (n_docs > 0 && !docs)) return fail(c, KVR_E_ARG, "kvr_repair: bad document array");
+// Shared body of kvr_repair (bits 0) and kvr_repair_packed.
+static kvr_status repair(kvr_ctx *c, const char *name, const kvr_doc *docs, int32_t n_docs, int32_t bits, void *stream) {
+    const std::string who = name;
+    if (!c) return fail(nullptr, KVR_E_ARG, who + ": NULL context");
+    if (n_docs < 0 || (n_docs > 0 && !docs)) return fail(c, KVR_E_ARG, who + ": bad document array");
     long long total = 0;
     for (int i = 0; i < n_docs; ++i) {
         const kvr_doc &dc = docs[i];
-        const std::string tag = "kvr_repair: document " + std::to_string(i) + ": ";
+        const std::string tag = who + ": document " + std::to_string(i) + ": ";
         if (dc.n_positions < 0 || (dc.n_positions > 0 && !dc.h_positions))
             return fail(c, KVR_E_ARG, tag + "bad position list");
         if (dc.n < 1 || dc.n > dc.n_cap || dc.n_cap > c->d.max_ctx)
@@ -1346,7 +1586,7 @@ kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *str
         if (np > 0 && !aligned16(dc.d_cache)) return fail(c, KVR_E_ARG, tag + "cache must be 16-byte aligned");
         total += np;
     }
-    if (total > c->d.max_rows) return fail(c, KVR_E_RANGE, "kvr_repair: total |P| exceeds max_rows");
+    if (total > c->d.max_rows) return fail(c, KVR_E_RANGE, who + ": total |P| exceeds max_rows");
     if (total == 0) return KVR_OK;
     // Documents of one call are repaired in one pass: every document's fresh
     // rows of a layer are scattered before any row attends.  Two documents
@@ -1358,12 +1598,12 @@ kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *str
             const kvr_doc &dc = docs[i];
             if ((dc.edit_end - dc.edit_start) + dc.n_positions == 0) continue;
             const uintptr_t b = (uintptr_t)dc.d_cache;
-            spans.push_back({b, b + kvr_cache_bytes(&c->d, dc.n_cap)});
+            spans.push_back({b, b + (bits ? packed_bytes(c->d, dc.n_cap, bits) : kvr_cache_bytes(&c->d, dc.n_cap))});
         }
         std::sort(spans.begin(), spans.end());
         for (size_t i = 1; i < spans.size(); ++i)
             if (spans[i].first < spans[i - 1].second)
-                return fail(c, KVR_E_ARG, "kvr_repair: two documents share cache memory");
+                return fail(c, KVR_E_ARG, who + ": two documents share cache memory");
     }
 
     Tables &t = c->tab;
@@ -1384,7 +1624,264 @@ kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *str
         while (j < dc.n_positions) t.rows.push_back(RowInfo{dc.h_positions[j++], di, out++, 0});
     }
     DeviceGuard g(c->device);
-    return run_pass(c, t, (hipStream_t)stream);
+    return run_pass(c, t, (hipStream_t)stream, -1, nullptr, false, bits);
+}
+
+kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *stream) {
+    return repair(c, "kvr_repair", docs, n_docs, 0, stream);
+}
+
+// ---- packed caches
+
+size_t kvr_packed_bytes(const kvr_dims *d, int32_t n_cap, int32_t bits) {
+    if (!d || n_cap < 0 || (bits != 4 && bits != 8) || check_dims(d) != KVR_OK) return 0;
+    return packed_bytes(*d, n_cap, bits);
+}
+
+typedef std::pair<uintptr_t, uintptr_t> Span;
+static bool spans_meet(std::vector<Span> &v) {
+    std::sort(v.begin(), v.end());
+    for (size_t i = 1; i < v.size(); ++i)
+        if (v[i].first < v[i - 1].second) return true;
+    return false;
+}
+
+// Shared body of kvr_pack and kvr_unpack.
+static kvr_status copy_packed(kvr_ctx *c, const char *name, const kvr_pack_doc *docs, int32_t n_docs, int32_t bits, bool unpack,
+                              void *stream) {
+    const std::string who = name;
+    if (!c) return fail(nullptr, KVR_E_ARG, who + ": NULL context");
+    kvr_status st = check_bits(c, name, bits);
+    if (st != KVR_OK) return st;
+    if (n_docs < 0 || (n_docs > 0 && !docs)) return fail(c, KVR_E_ARG, who + ": bad document array");
+    const size_t row = (size_t)c->d.head_dim * elem_size(c->d);
+    const int planes = c->d.n_layers * 2 * c->d.n_kv_heads;
+    std::vector<Span> written, read;
+    for (int i = 0; i < n_docs; ++i) {
+        const kvr_pack_doc &dc = docs[i];
+        auto bad = [&](kvr_status code, const char *what) {
+            return fail(c, code, who + ": document " + std::to_string(i) + ": " + what);
+        };
+        if (dc.n_positions < 0) return bad(KVR_E_ARG, "bad position list");
+        if (dc.n_positions == 0) continue;
+        if (!dc.d_cache || !dc.d_packed) return bad(KVR_E_ARG, "NULL cache");
+        if (!aligned16(dc.d_cache) || !aligned16(dc.d_packed)) return bad(KVR_E_ARG, "caches must be 16-byte aligned");
+        const int32_t lim = std::min(dc.n_cap, dc.packed_n_cap);
+        if (!dc.h_positions && dc.n_positions > lim) return bad(KVR_E_RANGE, "more positions than a cache has slots");
+        if (dc.h_positions) st = check_positions(bad, dc.h_positions, dc.n_positions, 0, lim, true);
+        if (st != KVR_OK) return st;
+        const Span plain{(uintptr_t)dc.d_cache, (uintptr_t)dc.d_cache + (size_t)planes * dc.n_cap * row};
+        const Span packed{(uintptr_t)dc.d_packed, (uintptr_t)dc.d_packed + packed_bytes(c->d, dc.packed_n_cap, bits)};
+        written.push_back(unpack ? plain : packed);
+        read.push_back(unpack ? packed : plain);
+    }
+    if (written.empty()) return KVR_OK;
+    if (spans_meet(written)) return fail(c, KVR_E_ARG, who + ": two documents write the same memory");
+    for (const Span &r : read) {  // `written` is sorted and disjoint: the last span that starts before r ends
+        auto it = std::lower_bound(written.begin(), written.end(), Span{r.second, 0});
+        if (it != written.begin() && std::prev(it)->second > r.first)
+            return fail(c, KVR_E_ARG, who + ": a cache that is read is written too");
+    }
+    DeviceGuard g(c->device);
+    PackedTable table;
+    TableFill fill(&table);
+    int rows = 0;
+    auto flush = [&] {
+        const hipError_t e = launch_packed_copy(c->bf16, bits, unpack, table, fill.docs, rows, planes, c->d.n_kv_heads,
+                                                c->d.head_dim, (hipStream_t)stream);
+        fill = TableFill(&table);
+        rows = 0;
+        return e;
+    };
+    for (int i = 0; i < n_docs; ++i) {
+        const kvr_pack_doc &dc = docs[i];
+        for (int done = 0; done < dc.n_positions;) {
+            const int before = fill.docs;
+            static const int32_t none = 0;
+            int n;
+            if (dc.h_positions) {
+                n = fill.add(dc.d_packed, pk_blocks(dc.packed_n_cap), rows, dc.h_positions + done, 1, dc.n_positions - done, true,
+                             false);
+            } else {
+                n = fill.add(dc.d_packed, pk_blocks(dc.packed_n_cap), rows, &none, 1, 1, true, false);
+                if (n) {
+                    n = dc.n_positions;
+                    fill.entry(before)[PKE_ROWS] = (uint32_t)n;
+                }
+            }
+            if (n == 0) {
+                const hipError_t e = flush();
+                if (e != hipSuccess) return hip_fail(c, e, name);
+                continue;
+            }
+            uint32_t *e = fill.entry(before);
+            e[PKE_CACHE] = (uint32_t)(uintptr_t)dc.d_cache;
+            e[PKE_CACHE + 1] = (uint32_t)((uintptr_t)dc.d_cache >> 32);
+            e[PKE_NCAP] = (uint32_t)dc.n_cap;
+            rows += n;
+            done += n;
+        }
+    }
+    const hipError_t e = flush();
+    return e == hipSuccess ? KVR_OK : hip_fail(c, e, name);
+}
+
+kvr_status kvr_pack(kvr_ctx *c, const kvr_pack_doc *docs, int32_t n_docs, int32_t bits, void *stream) {
+    return guarded(c, [&] { return copy_packed(c, "kvr_pack", docs, n_docs, bits, false, stream); });
+}
+
+kvr_status kvr_unpack(kvr_ctx *c, const kvr_pack_doc *docs, int32_t n_docs, int32_t bits, void *stream) {
+    return guarded(c, [&] { return copy_packed(c, "kvr_unpack", docs, n_docs, bits, true, stream); });
+}
+
+// What kvr_append_packed and kvr_attention_packed check alike; *rows: rows of all
+// documents.
+static kvr_status check_packed_rows(kvr_ctx *c, const char *name, int32_t layer, int32_t bits, const kvr_packed_rows *docs,
+                                    int32_t n_docs, bool append, int32_t *rows) {
+    const std::string who = name;
+    kvr_status st = check_bits(c, name, bits);
+    if (st != KVR_OK) return st;
+    if (layer < 0 || layer >= c->d.n_layers) return fail(c, KVR_E_RANGE, who + ": layer out of range");
+    if (n_docs < 0 || (n_docs > 0 && !docs)) return fail(c, KVR_E_ARG, who + ": bad document array");
+    long long total = 0;
+    std::vector<Span> written;
+    for (int i = 0; i < n_docs; ++i) {
+        const kvr_packed_rows &dc = docs[i];
+        auto bad = [&](kvr_status code, const char *what) {
+            return fail(c, code, who + ": document " + std::to_string(i) + ": " + what);
+        };
+        if (dc.n_rows < 0 || (dc.n_rows > 0 && !dc.h_positions)) return bad(KVR_E_ARG, "bad position list");
+        if (dc.n_rows == 0) continue;
+        if (!dc.d_packed || !aligned16(dc.d_packed)) return bad(KVR_E_ARG, "NULL cache, or not 16-byte aligned");
+        if (dc.n_cap < 1 || dc.n_cap > c->d.max_ctx) return bad(KVR_E_RANGE, "need 1 <= n_cap <= max_ctx");
+        st = check_positions(bad, dc.h_positions, dc.n_rows, append ? 0 : -1, dc.n_cap, append);
+        if (st != KVR_OK) return st;
+        total += dc.n_rows;
+        if (append) written.push_back({(uintptr_t)dc.d_packed, (uintptr_t)dc.d_packed + packed_bytes(c->d, dc.n_cap, bits)});
+    }
+    if (total * c->d.n_heads > 0x7fffffff) return fail(c, KVR_E_RANGE, who + ": too many rows");
+    if (spans_meet(written)) return fail(c, KVR_E_ARG, who + ": two documents share cache memory");
+    *rows = (int32_t)total;
+    return KVR_OK;
+}
+
+static bool aligned_to(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
+
+static kvr_status append_packed(kvr_ctx *c, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                                const void *d_k, const void *d_v, int64_t row_stride, void *stream) {
+    const char *const who = "kvr_append_packed";
+    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_append_packed: NULL context");
+    int32_t total = 0;
+    kvr_status st = check_packed_rows(c, who, layer, bits, docs, n_docs, true, &total);
+    if (st != KVR_OK || total == 0) return st;
+    const size_t es = elem_size(c->d);
+    if (!d_k || !d_v || !aligned_to(d_k, es) || !aligned_to(d_v, es))
+        return fail(c, KVR_E_ARG, "kvr_append_packed: NULL or misaligned keys or values");
+    if (row_stride < (int64_t)c->d.n_kv_heads * c->d.head_dim)
+        return fail(c, KVR_E_RANGE, "kvr_append_packed: row_stride below n_kv_heads * head_dim");
+    DeviceGuard g(c->device);
+    PackedTable table;
+    TableFill fill(&table);
+    int row = 0, first = 0;
+    auto flush = [&] {
+        const hipError_t e = launch_packed_append(c->bf16, bits, table, fill.docs, row - first, d_k, d_v, row_stride, layer,
+                                                  c->d.n_kv_heads, c->d.head_dim, (hipStream_t)stream);
+        fill = TableFill(&table);
+        first = row;
+        return e;
+    };
+    for (int i = 0; i < n_docs; ++i) {
+        const kvr_packed_rows &dc = docs[i];
+        for (int done = 0; done < dc.n_rows;) {
+            const int n = fill.add(dc.d_packed, pk_blocks(dc.n_cap), row, dc.h_positions + done, 1, dc.n_rows - done, true, false);
+            if (n == 0) {
+                const hipError_t e = flush();
+                if (e != hipSuccess) return hip_fail(c, e, who);
+                continue;
+            }
+            row += n;
+            done += n;
+        }
+    }
+    const hipError_t e = flush();
+    return e == hipSuccess ? KVR_OK : hip_fail(c, e, who);
+}
+
+kvr_status kvr_append_packed(kvr_ctx *c, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                             const void *d_k, const void *d_v, int64_t row_stride, void *stream) {
+    return guarded(c, [&] { return append_packed(c, layer, bits, docs, n_docs, d_k, d_v, row_stride, stream); });
+}
+
+static kvr_status attention_packed(kvr_ctx *c, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                                   const void *d_q, int64_t q_stride, void *d_out, int64_t out_stride, void *stream) {
+    if (!c) return fail(nullptr, KVR_E_ARG, "kvr_attention_packed: NULL context");
+    int32_t total = 0;
+    kvr_status st = check_packed_rows(c, "kvr_attention_packed", layer, bits, docs, n_docs, false, &total);
+    if (st != KVR_OK || total == 0) return st;
+    const size_t es = elem_size(c->d);
+    if (!d_q || !d_out || !aligned_to(d_q, es) || !aligned_to(d_out, es))
+        return fail(c, KVR_E_ARG, "kvr_attention_packed: NULL or misaligned queries or output");
+    const int64_t qd = (int64_t)c->d.n_heads * c->d.head_dim;
+    if (q_stride < qd || out_stride < qd)
+        return fail(c, KVR_E_RANGE, "kvr_attention_packed: a row stride is below n_heads * head_dim");
+    DeviceGuard g(c->device);
+    Tables &t = c->tab;
+    t.clear();
+    std::vector<int> row0(n_docs);
+    for (int i = 0, r = 0; i < n_docs; r += docs[i++].n_rows) row0[i] = r;
+    plan_packed(c, t, n_docs, [&](int i) {
+        return PackedQuery{docs[i].d_packed, docs[i].n_cap, row0[i], docs[i].n_rows, docs[i].h_positions, 1};
+    }, false);
+    PackedAttnArgs a{};
+    a.q = d_q; a.q_stride = q_stride;
+    a.out = d_out; a.out_stride = out_stride;
+    a.layer = layer;
+    for (const auto &l : t.packed) {
+        hipError_t e = launch_attention_packed(c->bf16, bits, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
+        if (e == hipSuccess && l.combine)
+            e = launch_attention_packed_combine(c->bf16, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(c, e, "kvr_attention_packed");
+    }
+    return KVR_OK;
+}
+
+kvr_status kvr_attention_packed(kvr_ctx *c, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,
+                                const void *d_q, int64_t q_stride, void *d_out, int64_t out_stride, void *stream) {
+    return guarded(c, [&] {
+        return attention_packed(c, layer, bits, docs, n_docs, d_q, q_stride, d_out, out_stride, stream);
+    });
+}
+
+// The decoder over packed caches.
+kvr_status kvr_prefill_packed(kvr_ctx *c, const int32_t *d_tokens, int32_t n, int32_t n_cap, void *d_packed, int32_t bits,
+                              float *d_hidden_out, void *stream) {
+    return guarded(c, [&] {
+        const kvr_status st = c ? check_bits(c, "kvr_prefill_packed", bits) : KVR_OK;
+        return st != KVR_OK ? st : prefill(c, "kvr_prefill_packed", d_tokens, n, n_cap, d_packed, bits, d_hidden_out, stream);
+    });
+}
+
+kvr_status kvr_repair_packed(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, int32_t bits, void *stream) {
+    return guarded(c, [&] {
+        const kvr_status st = c ? check_bits(c, "kvr_repair_packed", bits) : KVR_OK;
+        return st != KVR_OK ? st : repair(c, "kvr_repair_packed", docs, n_docs, bits, stream);
+    });
+}
+
+kvr_status kvr_score_packed(kvr_ctx *c, void *d_packed, int32_t bits, int32_t n, int32_t n_cap, const int32_t *d_tokens,
+                            int32_t m, float *d_logprob, int32_t *d_argmax, void *stream) {
+    return guarded(c, [&] {
+        const kvr_status st = c ? check_bits(c, "kvr_score_packed", bits) : KVR_OK;
+        return st != KVR_OK ? st : score(c, "kvr_score_packed", d_packed, bits, n, n_cap, d_tokens, m, d_logprob, d_argmax, stream);
+    });
+}
+
+kvr_status kvr_generate_packed(kvr_ctx *c, void *d_packed, int32_t bits, int32_t n, int32_t n_cap, int32_t *d_tokens, int32_t q,
+                               int32_t max_new, void *stream) {
+    return guarded(c, [&] {
+        const kvr_status st = c ? check_bits(c, "kvr_generate_packed", bits) : KVR_OK;
+        return st != KVR_OK ? st : generate(c, "kvr_generate_packed", d_packed, bits, n, n_cap, d_tokens, q, max_new, stream);
+    });
 }
 
 }  // extern "C"

@@ -1,0 +1,146 @@
+// Packed caches: a cache's rows in codes of 4 or 8 bits (layout and rounding are
+// stated in include/kvr.h).  Shared by the kernels that write, read and attend
+// over them.
+#pragma once
+
+#include "common.h"
+
+namespace kvr {
+
+constexpr int PK_BLOCK = 32;  // positions of a block
+constexpr int PK_GROUP = 64;  // dimensions that share a scale and an offset
+
+// head_dim as the codes hold it
+__host__ __device__ constexpr int pk_width(int hd) { return hd <= 64 ? 64 : 128; }
+// bytes of a block's codes, and of the block (codes, then a 32-bit word of scale
+// and offset per position and group)
+__host__ __device__ constexpr int pk_code_bytes(int hp, int bits) { return PK_BLOCK * hp * bits / 8; }
+__host__ __device__ constexpr int pk_block_bytes(int hp, int bits) {
+    return pk_code_bytes(hp, bits) + PK_BLOCK * (hp / PK_GROUP) * 4;
+}
+__host__ __device__ constexpr int pk_blocks(int n_cap) { return (n_cap + PK_BLOCK - 1) / PK_BLOCK; }
+
+// Byte of the code of (position r of the block, dimension d), and the bit it
+// starts at.  Keys: 16-position tiles, in each [8-dimension group of a step of
+// 32][position][step], eight dimensions side by side: what a lane of the score
+// product's A operand reads.  Values: [group of four positions][dimension of
+// 16][16 dimensions, in 4 bits paired][half of the block], four positions side by
+// side: what a lane of the output product's A operand reads.
+__host__ __device__ __forceinline__ int pk_key_byte(int hp, int bits, int r, int d, int *bit) {
+    const int word = (((r >> 4) * 4 + ((d >> 3) & 3)) * 16 + (r & 15)) * (hp >> 5) + (d >> 5);
+    const int j = d & 7;
+    if (bits == 8) {
+        *bit = 0;
+        return word * 8 + j;
+    }
+    const int nib = (j & 1) * 4 + (j >> 1);  // even dimensions in the low half, odd ones in the high half
+    *bit = 4 * (nib & 1);
+    return word * 4 + (nib >> 1);
+}
+__host__ __device__ __forceinline__ int pk_value_byte(int hp, int bits, int r, int d, int *bit) {
+    const int lane = ((r >> 2) & 3) * 16 + (d & 15);
+    if (bits == 8) {
+        *bit = 0;
+        return ((lane * (hp >> 4) + (d >> 4)) * 2 + (r >> 4)) * 4 + (r & 3);
+    }
+    *bit = 4 * ((d >> 4) & 1);
+    return ((lane * (hp >> 5) + (d >> 5)) * 2 + (r >> 4)) * 4 + (r & 3);
+}
+
+// The documents and positions of one launch, in the kernel's argument (HIP's
+// limit is 4 KB), so that a call stages nothing in memory and a captured one
+// keeps its own.  Entries of PK_ENTRY words stand at the front, positions at the
+// back.
+constexpr int PK_WORDS = 896, PK_ENTRY = 12;
+constexpr int PK_MAX_DOCS = PK_WORDS / PK_ENTRY;
+struct PackedTable {
+    uint32_t w[PK_WORDS];
+};
+// Words of an entry.  Rows r of an entry are rows ROW0 + r of the launch's row
+// arrays; their positions are POS + r (POS >= 0 or -1) when REF is
+// PK_RUN, word REF + r of the table, or, when REF is PK_ROWS, those of the pass's
+// row table.
+enum {
+    PKE_PACKED = 0,  // packed cache (two words)
+    PKE_BLOCKS = 2,  // its blocks per plane
+    PKE_ROW0 = 3,
+    PKE_ROWS = 4,
+    PKE_REF = 5,
+    PKE_POS = 6,
+    // attention: first work item and column group of the entry in the launch, key
+    // ranges per column group, first partial slot, keys that a row sees at most
+    PKE_ITEM0 = 7,
+    PKE_CG0 = 8,
+    PKE_SPLITS = 9,
+    PKE_PART0 = 10,
+    PKE_KEYS = 11,
+    // copies: the cache (two words) and its rows per plane
+    PKE_CACHE = 7,
+    PKE_NCAP = 9,
+};
+constexpr uint32_t PK_RUN = 0xffffffffu, PK_ROWS = 0xfffffffeu;
+
+// Quantise the listed rows of k and v ([rows][stride] values, heads side by side)
+// into one layer's planes of the entries' packed caches.
+hipError_t launch_packed_append(bool bf16, int bits, const PackedTable &t, int n_docs, int n_rows, const void *k,
+                                const void *v, int64_t stride, int layer, int Hkv, int hd, hipStream_t s);
+// Quantise (unpack: read back) the listed positions of every plane.
+hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTable &t, int n_docs, int n_rows, int planes,
+                              int Hkv, int hd, hipStream_t s);
+// launch_rope_scatter for packed caches: the fresh keys (after the rotation) and
+// values are quantised into their documents' caches; q is written row-major.
+hipError_t launch_rope_pack(bool bf16, int bits, const float *qkv, int nsplit, const void *bq, const void *bk,
+                            const void *bv, const RowInfo *rows, const DocInfo *docs, int R, int layer, int Hq, int Hkv,
+                            int hd, const float *rope_cos, const float *rope_sin, void *Q, void *Q_lo, hipStream_t s);
+
+// One attention launch and its combine (attention_packed.h).
+struct PackedAttnArgs {
+    const void *q, *q_lo;   // [rows][q_stride]; q_lo: low parts of a compensated pair, or null
+    int64_t q_stride;
+    void *out, *out_lo;     // [rows][out_stride], or operand order (o_perm)
+    int64_t out_stride;
+    int32_t o_perm;
+    const RowInfo *rows;    // the pass's row table (PK_ROWS), or null
+    float *part;
+    int32_t layer, Hq, Hkv, hd;
+    int32_t n_docs, n_items, n_cg;
+    int32_t range;          // keys of a key range (a multiple of PK_BLOCK)
+};
+// Columns (row, query head of the kv head's group) of a column group: nt 16-column
+// tiles for each of cw wavefronts; the block's 4 / cw wavefronts of a tile take
+// alternate key blocks.
+struct PackedShape { int nt, cw; };
+constexpr int pk_cols(PackedShape s) { return 16 * s.nt * s.cw; }
+constexpr int PK_ATT_WAVES = 4;
+constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
+hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
+                                   hipStream_t s);
+hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
+                                           hipStream_t s);
+
+#ifdef __HIPCC__
+// Entry of a launch that holds index `x`: the last one whose word `word` is not
+// above it.  Every lane looks at one entry, so the search is one load deep.
+__device__ __forceinline__ int pk_find(const PackedTable &t, int n_docs, int word, int x) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+#pragma unroll
+    for (int b = 0; b < (PK_MAX_DOCS + 63) / 64; ++b) {
+        const int i = b * 64 + lane;
+        n += __popcll(__ballot(i < n_docs && (int)t.w[i * PK_ENTRY + word] <= x));
+    }
+    return __builtin_amdgcn_readfirstlane(n - 1);
+}
+__device__ __forceinline__ char *pk_pointer(const uint32_t *e) {
+    return (char *)(((uint64_t)e[1] << 32) | e[0]);
+}
+// Position of row r of entry e.
+__device__ __forceinline__ int pk_position(const PackedTable &t, const uint32_t *e, int r, const RowInfo *rows) {
+    const uint32_t ref = e[PKE_REF];
+    if (ref == PK_RUN) return (int)e[PKE_POS] + r;
+    if (ref == PK_ROWS) return rows[e[PKE_ROW0] + r].pos;
+    return (int)t.w[ref + r];
+}
+#endif
+
+}  // namespace kvr
