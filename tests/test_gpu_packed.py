@@ -7,7 +7,7 @@ import torch
 
 import paper_2609_17983_amd as kvr
 from tests import packed_ref as ref
-from tests.gpu_util import say
+from tests.gpu_util import TOL, say
 
 pytestmark = pytest.mark.gpu
 
@@ -243,7 +243,7 @@ def check_attention(c, bits, docs, packs, decs, q_extra=0, o_extra=0, q_off=0, o
     assert (body[:, Hq * hd:] == 3.0).all()
     y = body[:, :Hq * hd].float().numpy().reshape(R, Hq, hd).astype(np.float64)
     qn = x[:, :Hq * hd].reshape(R, Hq, hd)
-    at, worst = 0, 0.0
+    at, worst, full = 0, 0.0, np.zeros_like(y)
     half = torch.finfo(TDT[c.dtype]).eps / 2
     for i, pos in docs:
         kc, vc = decs[i]
@@ -251,11 +251,15 @@ def check_attention(c, bits, docs, packs, decs, q_extra=0, o_extra=0, q_off=0, o
         want = ref.attend(qq, pos, ref.values(*kc), ref.values(*vc))
         tol = ref.attend_bound(qq, pos, kc, vc, bits, c.dtype == F32)[..., None] * (1 + half) + half * np.abs(want) + 1e-30
         diff = np.abs(y[at:at + len(pos)] - want)
+        full[at:at + len(pos)] = want
         assert np.array_equal(np.isnan(diff), np.isnan(want))
         worst = max(worst, float(np.nan_to_num(diff / tol).max(initial=0.0)))
         at += len(pos)
-    say(f"attention {bits} bits hd={hd} Hq={Hq}/{c.Hkv} rows={R}: worst error over bound {worst:.3f}")
-    assert worst <= 1.0
+    # and over all of them: the output's rounding alone in bf16, the repository's tolerance in fp32
+    ok = np.isfinite(full)
+    rel = float(np.linalg.norm(y[ok] - full[ok]) / max(np.linalg.norm(full[ok]), 1e-300))
+    say(f"attention {bits} bits hd={hd} Hq={Hq}/{c.Hkv} rows={R}: worst error over bound {worst:.3f}, of all {rel:.2e}")
+    assert worst <= 1.0 and rel <= (TOL[F32] if c.dtype == F32 else half)
     return body
 
 
