@@ -563,6 +563,48 @@ struct TableFill {
         e[PKE_POS] = (uint32_t)pos[0];
         return k;
     }
+    // An entry of a copy for the first of n ascending positions (null: 0 .. n - 1), as a
+    // run or as blocks with masks: *taken positions in *units blocks; null when the
+    // table is full.  Runs of two blocks' length or more get entries of their own.
+    uint32_t *add_units(const int32_t *pos, int n, int unit0, int *taken, int *units) {
+        const int room = tail - (docs + 1) * PK_ENTRY;
+        if (room < 0) return nullptr;
+        auto run = [&](int i) {
+            int j = i + 1;
+            while (j < n && pos[j] == pos[j - 1] + 1) ++j;
+            return j - i;
+        };
+        const int p0 = pos ? pos[0] : 0, k = pos ? run(0) : n;
+        uint32_t *e = entry(docs);
+        e[PKC_UNIT0] = (uint32_t)unit0;
+        e[PKE_POS] = (uint32_t)p0;
+        if (k == n || k >= 2 * PK_BLOCK) {
+            e[PKE_REF] = PK_RUN;
+            e[PKC_RUN] = (uint32_t)k;
+            *taken = k;
+            *units = (p0 + k - 1) / PK_BLOCK - p0 / PK_BLOCK + 1;
+        } else {
+            // the pairs are written downwards from the tail: units in descending order of blocks
+            int m = 0, i = 0;
+            while (i < n) {
+                if (pos[i] % PK_BLOCK == 0 && run(i) >= 2 * PK_BLOCK) break;
+                if (2 * (m + 1) > room) break;
+                const int b = pos[i] / PK_BLOCK;
+                uint32_t mask = 0;
+                for (; i < n && pos[i] / PK_BLOCK == b; ++i) mask |= 1u << pos[i] % PK_BLOCK;
+                ++m;
+                t->w[tail - 2 * m] = (uint32_t)b;
+                t->w[tail - 2 * m + 1] = mask;
+            }
+            if (m == 0) return nullptr;
+            tail -= 2 * m;
+            e[PKE_REF] = (uint32_t)tail;
+            *taken = i;
+            *units = m;
+        }
+        ++docs;
+        return e;
+    }
 };
 
 // The query rows of one document: positions `step` words apart.
@@ -1685,40 +1727,31 @@ static kvr_status copy_packed(kvr_ctx *c, const char *name, const kvr_pack_doc *
     DeviceGuard g(c->device);
     PackedTable table;
     TableFill fill(&table);
-    int rows = 0;
+    int units = 0;
     auto flush = [&] {
-        const hipError_t e = launch_packed_copy(c->bf16, bits, unpack, table, fill.docs, rows, planes, c->d.n_kv_heads,
+        const hipError_t e = launch_packed_copy(c->bf16, bits, unpack, table, fill.docs, units, planes, c->d.n_kv_heads,
                                                 c->d.head_dim, (hipStream_t)stream);
         fill = TableFill(&table);
-        rows = 0;
+        units = 0;
         return e;
     };
     for (int i = 0; i < n_docs; ++i) {
         const kvr_pack_doc &dc = docs[i];
         for (int done = 0; done < dc.n_positions;) {
-            const int before = fill.docs;
-            static const int32_t none = 0;
-            int n;
-            if (dc.h_positions) {
-                n = fill.add(dc.d_packed, pk_blocks(dc.packed_n_cap), rows, dc.h_positions + done, 1, dc.n_positions - done, true,
-                             false);
-            } else {
-                n = fill.add(dc.d_packed, pk_blocks(dc.packed_n_cap), rows, &none, 1, 1, true, false);
-                if (n) {
-                    n = dc.n_positions;
-                    fill.entry(before)[PKE_ROWS] = (uint32_t)n;
-                }
-            }
-            if (n == 0) {
-                const hipError_t e = flush();
-                if (e != hipSuccess) return hip_fail(c, e, name);
+            int n = 0, added = 0;
+            uint32_t *e = fill.add_units(dc.h_positions ? dc.h_positions + done : nullptr, dc.n_positions - done, units, &n, &added);
+            if (!e) {
+                const hipError_t err = flush();
+                if (err != hipSuccess) return hip_fail(c, err, name);
                 continue;
             }
-            uint32_t *e = fill.entry(before);
-            e[PKE_CACHE] = (uint32_t)(uintptr_t)dc.d_cache;
-            e[PKE_CACHE + 1] = (uint32_t)((uintptr_t)dc.d_cache >> 32);
-            e[PKE_NCAP] = (uint32_t)dc.n_cap;
-            rows += n;
+            e[PKE_PACKED] = (uint32_t)(uintptr_t)dc.d_packed;
+            e[PKE_PACKED + 1] = (uint32_t)((uintptr_t)dc.d_packed >> 32);
+            e[PKE_BLOCKS] = (uint32_t)pk_blocks(dc.packed_n_cap);
+            e[PKC_CACHE] = (uint32_t)(uintptr_t)dc.d_cache;
+            e[PKC_CACHE + 1] = (uint32_t)((uintptr_t)dc.d_cache >> 32);
+            e[PKC_NCAP] = (uint32_t)dc.n_cap;
+            units += added;
             done += n;
         }
     }

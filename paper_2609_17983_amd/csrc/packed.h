@@ -74,9 +74,14 @@ enum {
     PKE_SPLITS = 9,
     PKE_PART0 = 10,
     PKE_KEYS = 11,
-    // copies: the cache (two words) and its rows per plane
-    PKE_CACHE = 7,
-    PKE_NCAP = 9,
+    // copies: the units (blocks with listed positions) of the entry, by the first one's
+    // index in the launch; POS and RUN are a run of positions, otherwise word REF + 2 i
+    // is unit i's block and the next one the mask of its positions; the cache (two
+    // words) and its rows per plane
+    PKC_UNIT0 = 3,
+    PKC_CACHE = 7,
+    PKC_NCAP = 9,
+    PKC_RUN = 10,
 };
 constexpr uint32_t PK_RUN = 0xffffffffu, PK_ROWS = 0xfffffffeu;
 
@@ -85,7 +90,7 @@ constexpr uint32_t PK_RUN = 0xffffffffu, PK_ROWS = 0xfffffffeu;
 hipError_t launch_packed_append(bool bf16, int bits, const PackedTable &t, int n_docs, int n_rows, const void *k,
                                 const void *v, int64_t stride, int layer, int Hkv, int hd, hipStream_t s);
 // Quantise (unpack: read back) the listed positions of every plane.
-hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTable &t, int n_docs, int n_rows, int planes,
+hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTable &t, int n_docs, int n_units, int planes,
                               int Hkv, int hd, hipStream_t s);
 // launch_rope_scatter for packed caches: the fresh keys (after the rotation) and
 // values are quantised into their documents' caches; q is written row-major.

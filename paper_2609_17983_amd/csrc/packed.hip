@@ -18,6 +18,9 @@ namespace kvr {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
 __device__ __forceinline__ float wave_min(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fminf(v, __shfl_xor(v, o, 64));
@@ -29,8 +32,8 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// Scale and offset of a group of finite values within [lo, hi] (not `good`: one of
-// them is not finite), and the reciprocal that its codes are made with.
+// Scale and offset of a group of values within [lo, hi] (not `good`, or lo or hi not
+// finite: one of them is not), and the reciprocal that its codes are made with.
 template <int BITS>
 __device__ __forceinline__ uint32_t group_word(float lo, float hi, bool good, float *off, float *inv) {
     const uint32_t u = __float_as_uint(lo);
@@ -50,11 +53,11 @@ __device__ __forceinline__ uint32_t group_word(float lo, float hi, bool good, fl
     *inv = s ? 1.0f / __uint_as_float(s) : 0.f;
     return m | (s >> 16);
 }
-template <int BITS>
-__device__ __forceinline__ uint32_t code_of(float x, float off, float inv) {
-    constexpr float top = (float)((1 << BITS) - 1);
-    return (uint32_t)fminf(fmaxf(rintf((x - off) * inv), 0.f), top);
-}
+// The code of x as a whole float.  It is within [0, 2^bits - 1] by itself: off <= x,
+// and 1 / inv is at least (hi - off) / (2^bits - 1) to within a few 2^-24.
+__device__ __forceinline__ float code_of(float x, float off, float inv) { return rintf((x - off) * inv); }
+// A whole float below 2^23 as the low bits of a word.
+__device__ __forceinline__ uint32_t low_bits(float c) { return __float_as_uint(c + 8388608.f); }
 
 // A wavefront writes one row: lane l holds dimensions l (x[0]) and, in rows held 128
 // wide, 64 + l (x[1]); dimensions from hd on are not read.  `block`: the position's
@@ -71,7 +74,7 @@ __device__ __forceinline__ void write_row(const float x[2], int hd, bool value, 
         float off, inv;
         const uint32_t word = group_word<BITS>(wave_min(real ? x[g] : INFINITY), wave_max(real ? x[g] : -INFINITY), good,
                                                &off, &inv);
-        uint32_t c = real && good && inv != 0.f ? code_of<BITS>(x[g], off, inv) : 0;
+        uint32_t c = real && inv != 0.f ? (uint32_t)code_of(x[g], off, inv) : 0;
         int bit;
         if (value) {
             const int at = pk_value_byte(HP, BITS, r, d, &bit);
@@ -107,34 +110,229 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedTable t, int n
     write_row<HP, BITS>(x, hd, value, base, p % PK_BLOCK);
 }
 
-// One wavefront per (position, plane) of a cache.
-template <typename T, int HP, int BITS, bool UNPACK>
-__global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_docs, int planes, int hd, int Hkv) {
-    constexpr int GS = HP / PK_GROUP, BB = pk_block_bytes(HP, BITS);
-    const int lane = threadIdx.x & 63, plane = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = (int)t.w[PKE_ROW0] + blockIdx.x;
-    const uint32_t *e = t.w + pk_find(t, n_docs, PKE_ROW0, row) * PK_ENTRY;
-    if (plane >= planes) return;
-    const int p = pk_position(t, e, row - (int)e[PKE_ROW0], nullptr);
-    char *block = pk_pointer(e) + ((size_t)plane * e[PKE_BLOCKS] + p / PK_BLOCK) * BB;
-    T *cache = (T *)pk_pointer(e + PKE_CACHE) + ((size_t)plane * e[PKE_NCAP] + p) * hd;
-    const bool value = plane / Hkv & 1;
-    const int r = p % PK_BLOCK;
-    if constexpr (UNPACK) {
+// ---- whole blocks
+//
+// A block of threads takes a unit: the listed positions (`mask`) of one 32-position
+// block of a plane; with rows held 64 wide it takes two.  HP / 16 lanes share a row,
+// lane j dimensions 32 (j/2) + 8 (j%2) .. +8 and the eight 16 further on, so that
+// the two halves of a value byte are in one lane and a key word is one lane's.  The
+// packed block is put together (or taken apart) in LDS and moves to and from memory
+// in one contiguous piece; where only some positions are listed, their words and
+// bytes move one by one and the others are not touched.
+struct PackedUnit {
+    char *block;     // the packed block
+    size_t row;      // index of the block's first position among the cache's rows
+    const uint32_t *e;
+    uint32_t mask;
+};
+__device__ __forceinline__ PackedUnit pk_unit(const PackedTable &t, int n_docs, int unit, int plane, int block_bytes) {
+    PackedUnit u;
+    u.e = t.w + pk_find(t, n_docs, PKC_UNIT0, unit) * PK_ENTRY;
+    const int i = unit - (int)u.e[PKC_UNIT0];
+    int b;
+    if (u.e[PKE_REF] == PK_RUN) {
+        const int p0 = u.e[PKE_POS], p1 = p0 + (int)u.e[PKC_RUN];
+        b = p0 / PK_BLOCK + i;
+        const int lo = max(p0 - b * PK_BLOCK, 0), hi = min(p1 - b * PK_BLOCK, PK_BLOCK);
+        u.mask = (0xffffffffu >> (32 - (hi - lo))) << lo;
+    } else {
+        b = t.w[u.e[PKE_REF] + 2 * i];
+        u.mask = t.w[u.e[PKE_REF] + 2 * i + 1];
+    }
+    u.block = pk_pointer(u.e) + ((size_t)plane * u.e[PKE_BLOCKS] + b) * block_bytes;
+    u.row = (size_t)plane * u.e[PKC_NCAP] + (size_t)b * PK_BLOCK;
+    return u;
+}
+
+// Eight values from dimension d on, zeros behind hd; vec: hd is a multiple of 8 (rows
+// are then 16-byte aligned).
+__device__ __forceinline__ void pk_load8(const float *p, int d, int hd, bool vec, float *x) {
+    if (vec) {
+        const bool in = d < hd;
 #pragma unroll
-        for (int g = 0; g < GS; ++g) {
-            const int d = g * PK_GROUP + lane;
-            if (d >= hd) continue;
-            int bit;
-            const int at = value ? pk_value_byte(HP, BITS, r, d, &bit) : pk_key_byte(HP, BITS, r, d, &bit);
-            const uint32_t c = ((uint32_t)(uint8_t)block[at] >> bit) & ((1u << BITS) - 1);
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(block + pk_code_bytes(HP, BITS) + (r * GS + g) * 4);
-            // exact product: 8 significant bits each
-            cache[d] = from_f32<T>(__uint_as_float(w & 0xffff0000u) + __uint_as_float(w << 16) * (float)c);
+        for (int q = 0; q < 2; ++q) {
+            const f32x4 v = in ? *reinterpret_cast<const f32x4 *>(p + d + 4 * q) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
         }
     } else {
-        const float x[2] = {lane < hd ? to_f32(cache[lane]) : 0.f, 64 + lane < hd ? to_f32(cache[64 + lane]) : 0.f};
-        write_row<HP, BITS>(x, hd, value, block, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = d + i < hd ? p[d + i] : 0.f;
+    }
+}
+__device__ __forceinline__ void pk_load8(const bf16_t *p, int d, int hd, bool vec, float *x) {
+    if (vec) {
+        const u32x4 v = d < hd ? *reinterpret_cast<const u32x4 *>(p + d) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = d + i < hd ? bf16_to_f32(p[d + i]) : 0.f;
+    }
+}
+__device__ __forceinline__ void pk_store8(float *p, int d, int hd, bool vec, const float *x) {
+    if (vec && d < hd) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            *reinterpret_cast<f32x4 *>(p + d + 4 * q) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+    } else if (!vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < hd) p[d + i] = x[i];
+    }
+}
+__device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, const float *x) {
+    if (vec && d < hd) {
+        u32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            v[q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * q], x[2 * q + 1]}, bf16x2));
+        *reinterpret_cast<u32x4 *>(p + d) = v;
+    } else if (!vec) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < hd) p[d + i] = f32_to_bf16(x[i]);
+    }
+}
+
+template <typename T, int HP, int BITS, bool UNPACK>
+__global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_docs, int n_units, int hd, int Hkv) {
+    constexpr int GS = HP / PK_GROUP, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
+    constexpr int TPR = HP / 16, TPU = PK_BLOCK * TPR, NU = 256 / TPU;  // lanes of a row, of a unit; units
+    __shared__ __attribute__((aligned(16))) char lds[NU][BB];
+    const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPU), lt = threadIdx.x % TPU;
+    const int r = lt / TPR, j = lt % TPR, d0 = 32 * (j >> 1) + 8 * (j & 1);
+    const int unit = min((int)blockIdx.x * NU + sub, n_units - 1);  // a last odd one is done twice, alike
+    const PackedUnit u = pk_unit(t, n_docs, unit, blockIdx.y, BB);
+    const bool value = blockIdx.y / Hkv & 1, vec = hd % 8 == 0, mine = u.mask >> r & 1;
+    T *row = (T *)pk_pointer(u.e + PKC_CACHE) + (u.row + r) * hd;
+    char *b = lds[sub];
+    uint32_t *words = reinterpret_cast<uint32_t *>(b);
+    uint32_t *par = reinterpret_cast<uint32_t *>(b + CB) + r * GS + j / 4;  // four lanes to a group
+    if constexpr (UNPACK) {
+        // slots that no call wrote are not used, though their block is loaded
+        for (int i = lt; i < BB / 16; i += TPU)
+            reinterpret_cast<u32x4 *>(b)[i] = reinterpret_cast<const u32x4 *>(u.block)[i];
+        __syncthreads();
+        if (!mine) return;
+        const float off = __uint_as_float(*par & 0xffff0000u), s = __uint_as_float(*par << 16);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                int bit;
+                const int at = value ? pk_value_byte(HP, BITS, r, d0 + 16 * q + i, &bit) : pk_key_byte(HP, BITS, r, d0 + 16 * q + i, &bit);
+                const uint32_t c = (value ? (uint32_t)(uint8_t)b[at] >> bit : words[at >> 2] >> (8 * (at & 3) + bit)) & ((1u << BITS) - 1);
+                x[i] = fmaf(s, (float)c, off);  // (the product is exact: 8 significant bits each)
+            }
+            pk_store8(row, d0 + 16 * q, hd, vec, x);
+        }
+    } else {
+        float x[2][8];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (mine) pk_load8(row, d0 + 16 * q, hd, vec, x[q]);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[q][i] = 0.f;
+        // the reductions keep a NaN (v_minimum3 / v_maximum3)
+        float lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (vec ? d0 + 16 * q < hd : true) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (vec || d0 + 16 * q + i < hd) {
+                        lo = __builtin_elementwise_minimum(lo, x[q][i]);
+                        hi = __builtin_elementwise_maximum(hi, x[q][i]);
+                    }
+            }
+#pragma unroll
+        for (int o = 1; o < 4; o *= 2) {
+            lo = __builtin_elementwise_minimum(lo, __shfl_xor(lo, o, 64));
+            hi = __builtin_elementwise_maximum(hi, __shfl_xor(hi, o, 64));
+        }
+        float off, inv;
+        const uint32_t word = group_word<BITS>(lo, hi, true, &off, &inv);
+        if ((j & 3) == 0) *par = word;
+        float c[2][8];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[q][i] = code_of(x[q][i], off, inv);
+        if (hd != HP) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (d0 + 16 * q + i >= hd) c[q][i] = 0.f;
+        }
+        if (inv == 0.f) {  // one value, or NaN
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) c[q][i] = 0.f;
+        }
+        // codes are put together as floats, which hold 16 bits of them exactly
+        if (value) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                int bit;
+                if constexpr (BITS == 4) {
+                    b[pk_value_byte(HP, BITS, r, d0 + i, &bit)] = (char)low_bits(c[0][i] + 16.f * c[1][i]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) b[pk_value_byte(HP, BITS, r, d0 + 16 * q + i, &bit)] = (char)low_bits(c[q][i]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                int bit;
+                uint32_t *w = words + (pk_key_byte(HP, BITS, r, d0 + 16 * q, &bit) >> 2);
+                // halves of a word: 4 bits, even and odd dimensions; 8 bits, pairs
+                if constexpr (BITS == 4) {
+                    uint32_t h[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        h[k] = low_bits(c[q][k] + 16.f * c[q][2 + k] + 256.f * c[q][4 + k] + 4096.f * c[q][6 + k]);
+                    w[0] = __builtin_amdgcn_perm(h[1], h[0], 0x05040100u);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        w[k] = __builtin_amdgcn_perm(low_bits(c[q][4 * k + 2] + 256.f * c[q][4 * k + 3]),
+                                                     low_bits(c[q][4 * k] + 256.f * c[q][4 * k + 1]), 0x05040100u);
+                }
+            }
+        }
+        __syncthreads();
+        if (u.mask == 0xffffffffu) {
+            for (int i = lt; i < BB / 16; i += TPU)
+                reinterpret_cast<u32x4 *>(u.block)[i] = reinterpret_cast<const u32x4 *>(b)[i];
+            return;
+        }
+        uint32_t *out = reinterpret_cast<uint32_t *>(u.block);
+        for (int i = lt; i < BB / 4; i += TPU) {
+            int at = i;  // word of a code
+            uint32_t m = 1;
+            if (i >= CB / 4) {
+                m = u.mask >> ((i - CB / 4) / GS) & 1;
+            } else if (!value) {
+                at /= (HP / 32) * (BITS / 4);  // [tile][lane group][position]
+                m = u.mask >> ((at >> 6) * 16 + (at & 15)) & 1;
+            } else {
+                const int h = i & 1, g = i / ((HP / 32) * (BITS / 4) * 2) / 16;  // [position group][dimension]
+                m = u.mask >> (16 * h + 4 * g) & 15;
+                if (m != 15) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (m >> k & 1) u.block[4 * i + k] = b[4 * i + k];
+                    continue;
+                }
+            }
+            if (m) out[i] = words[i];
+        }
     }
 }
 
@@ -210,20 +408,21 @@ hipError_t launch_packed_append(bool bf16, int bits, const PackedTable &t, int n
     return hipGetLastError();
 }
 
-hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTable &t, int n_docs, int n_rows, int planes,
+hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTable &t, int n_docs, int n_units, int planes,
                               int Hkv, int hd, hipStream_t s) {
-    if (n_rows <= 0) return hipSuccess;
+    if (n_units <= 0) return hipSuccess;
     if (n_docs < 1 || n_docs > PK_MAX_DOCS || hd > 128 || (bits != 4 && bits != 8)) return hipErrorInvalidValue;
-    const dim3 grid(n_rows, (planes + 3) / 4);
-#define KVR_CALL(HP, BITS)                                                                                           \
-    if (bf16 && unpack)                                                                                              \
-        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, planes, hd, Hkv); \
-    else if (bf16)                                                                                                   \
-        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, planes, hd, Hkv); \
-    else if (unpack)                                                                                                 \
-        kvr_launch((packed_copy_kernel<float, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, planes, hd, Hkv);  \
-    else                                                                                                             \
-        kvr_launch((packed_copy_kernel<float, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, planes, hd, Hkv)
+    const int units = pk_width(hd) == 64 ? 2 : 1;
+    const dim3 grid((n_units + units - 1) / units, planes);
+#define KVR_CALL(HP, BITS)                                                                                             \
+    if (bf16 && unpack)                                                                                                \
+        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv);  \
+    else if (bf16)                                                                                                     \
+        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv); \
+    else if (unpack)                                                                                                   \
+        kvr_launch((packed_copy_kernel<float, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv);   \
+    else                                                                                                               \
+        kvr_launch((packed_copy_kernel<float, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv)
     KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
 #undef KVR_CALL
     return hipGetLastError();
