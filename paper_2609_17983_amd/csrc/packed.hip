@@ -187,7 +187,9 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             v[q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * q], x[2 * q + 1]}, bf16x2));
-        *reinterpret_cast<u32x4 *>(p + d) = v;
+        // a line leaves in one instruction and is not read again here: past the caches
+        // (28 layers of 4-bit codes, 5000 positions: 84 -> 61 us, 6.0 TB/s)
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p + d));
     } else if (!vec) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -215,18 +217,22 @@ __global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_d
             reinterpret_cast<u32x4 *>(b)[i] = reinterpret_cast<const u32x4 *>(u.block)[i];
         __syncthreads();
         if (!mine) return;
-        const float off = __uint_as_float(*par & 0xffff0000u), s = __uint_as_float(*par << 16);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
+            // here a lane takes the eight dimensions 8 j + q HP / 2, so that a store instruction
+            // writes whole lines
+            const int d1 = q * (HP / 2) + 8 * j;
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(b + CB + (r * GS + d1 / PK_GROUP) * 4);
+            const float off = __uint_as_float(w & 0xffff0000u), s = __uint_as_float(w << 16);
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 int bit;
-                const int at = value ? pk_value_byte(HP, BITS, r, d0 + 16 * q + i, &bit) : pk_key_byte(HP, BITS, r, d0 + 16 * q + i, &bit);
+                const int at = value ? pk_value_byte(HP, BITS, r, d1 + i, &bit) : pk_key_byte(HP, BITS, r, d1 + i, &bit);
                 const uint32_t c = (value ? (uint32_t)(uint8_t)b[at] >> bit : words[at >> 2] >> (8 * (at & 3) + bit)) & ((1u << BITS) - 1);
                 x[i] = fmaf(s, (float)c, off);  // (the product is exact: 8 significant bits each)
             }
-            pk_store8(row, d0 + 16 * q, hd, vec, x);
+            pk_store8(row, d1, hd, vec, x);
         }
     } else {
         float x[2][8];
