@@ -37,6 +37,8 @@
 // are split over blocks leave partials (O, m, l) that a combine kernel joins.
 #include <math.h>
 
+#include <type_traits>
+
 #include "packed.h"
 
 namespace kvr {
@@ -211,12 +213,24 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
     const int kvh = blockIdx.y;
     const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.x) * PK_ENTRY;
     const int nsplit = e[PKE_SPLITS], item = blockIdx.x - (int)e[PKE_ITEM0];
-    const int ncols_doc = (int)e[PKE_ROWS] * (a.Hq / a.Hkv), G = a.Hq / a.Hkv;
     const int cols = 16 * NT * cw;
+    const int kw = PK_ATT_WAVES / cw, wk = w / cw, wc = w - wk * cw;
+    const int split = nsplit == 1 ? 0 : item % nsplit;
+    // the first key block's loads wait for nothing else
+    const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
+    const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
+    const char *vp = kp + a.Hkv * plane;
+    const int b0 = split * (a.range / PK_BLOCK) + wk;
+    PackedBlock<HP, BITS> kb, vb;
+    {
+        const size_t first = (size_t)min(b0, (int)e[PKE_BLOCKS] - 1) * BB;
+        kb.load_keys(kp + first, lane);
+        vb.load_values(vp + first, lane);
+    }
+    const int G = a.Hq / a.Hkv, ncols_doc = (int)e[PKE_ROWS] * G;
     // column groups from the last one down: later rows see more keys
     const int ncg = (ncols_doc + cols - 1) / cols;
-    const int split = item % nsplit, cg = ncg - 1 - item / nsplit;
-    const int kw = PK_ATT_WAVES / cw, wk = w / cw, wc = w - wk * cw;
+    const int cg = ncg - 1 - (nsplit == 1 ? item : item / nsplit);
     const int row0 = e[PKE_ROW0];
 
     // this lane's columns: their row, head and number of visible keys
@@ -238,36 +252,60 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
         const T *q = (const T *)a.q + q0;
 #pragma unroll
         for (int g = 0; g < GS; ++g) qsum[n][g] = 0.f;
+        if constexpr (QP <= 2) {
+            u32x4 u[QP][KS];
+            if (q_vec) {  // hd is a multiple of 8
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int d = 32 * s + 8 * g4;
-            if constexpr (QP <= 2) {
+                for (int x = 0; x < QP; ++x)
 #pragma unroll
-                for (int x = 0; x < QP; ++x) {
-                    const T *src = x ? (const T *)a.q_lo + q0 : q;
-                    u32x4 u = {0, 0, 0, 0};
-                    if (q_vec) {
-                        if (d < a.hd) u = *reinterpret_cast<const u32x4 *>(src + d);
-                    } else {
+                    for (int s = 0; s < KS; ++s)
+                        u[x][s] = *reinterpret_cast<const u32x4 *>((x ? (const T *)a.q_lo + q0 : q) + min(32 * s + 8 * g4, a.hd - 8));
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (d + j < a.hd) u[j >> 1] |= (uint32_t)src[d + j] << (16 * (j & 1));
+                for (int x = 0; x < QP; ++x)
+#pragma unroll
+                    for (int s = 0; s < KS; ++s)
+                        if (32 * s + 8 * g4 >= a.hd) u[x][s] = u32x4{0, 0, 0, 0};
+            } else {
+#pragma unroll
+                for (int x = 0; x < QP; ++x)
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        u[x][s] = u32x4{0, 0, 0, 0};
+                        for (int j = 0; j < 8; ++j) {
+                            const int d = 32 * s + 8 * g4 + j;
+                            const uint32_t v = d < a.hd ? (uint32_t)(x ? (const T *)a.q_lo + q0 : q)[d] : 0;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (k == j >> 1) u[x][s][k] |= v << (16 * (j & 1));
+                        }
                     }
-                    qv[n][x][s] = __builtin_bit_cast(bf16x8, u);
+            }
+#pragma unroll
+            for (int x = 0; x < QP; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    qv[n][x][s] = __builtin_bit_cast(bf16x8, u[x][s]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        qsum[n][s / 2] += __uint_as_float(u[j] << 16) + __uint_as_float(u[j] & 0xffff0000u);
+                        qsum[n][s / 2] += __uint_as_float(u[x][s][j] << 16) + __uint_as_float(u[x][s][j] & 0xffff0000u);
                 }
-            } else {
-                float v[8];
+        } else {
+            float v[KS][8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = d + j < a.hd ? (float)q[d + j] : 0.f;
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[s][j] = (float)q[min(32 * s + 8 * g4 + j, a.hd - 1)];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (32 * s + 8 * g4 + j >= a.hd) v[s][j] = 0.f;
+                    qsum[n][s / 2] += v[s][j];
+                }
                 bf16x8 p[QP];
-                pk_pieces<QP>(v, p);
+                pk_pieces<QP>(v[s], p);
 #pragma unroll
                 for (int x = 0; x < QP; ++x) qv[n][x][s] = p[x];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) qsum[n][s / 2] += v[j];
             }
         }
 #pragma unroll
@@ -281,6 +319,8 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
     }
     top = __builtin_amdgcn_readfirstlane(top);
     least = __builtin_amdgcn_readfirstlane(least);
+    const int b1 = (min(top, (split + 1) * a.range) + PK_BLOCK - 1) / PK_BLOCK;
+    const int b_full = min(b1, least / PK_BLOCK);  // blocks before it need no mask
 
     f32x4 o[NT][DT];
     float m[NT], l[NT], z[NT][GS];
@@ -294,26 +334,16 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
         l[n] = 0.f;
     }
     const float sc = 1.4426950408889634f / sqrtf((float)a.hd);
-    const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
-    const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
-    const char *vp = kp + a.Hkv * plane;
-    const int b0 = split * (a.range / PK_BLOCK) + wk;
-    const int b1 = (min(top, (split + 1) * a.range) + PK_BLOCK - 1) / PK_BLOCK;
 
-    PackedBlock<HP, BITS> kb, vb;
-    if (b0 < b1) {
-        kb.load_keys(kp + (size_t)b0 * BB, lane);
-        vb.load_values(vp + (size_t)b0 * BB, lane);
-    }
-#pragma unroll 1
-    for (int b = b0; b < b1; b += kw) {
+    // one block of keys; masked: a column may not see all of them
+    auto step = [&](int b, auto masked_) {
+        constexpr bool MASKED = decltype(masked_)::value;
         const PackedBlock<HP, BITS> kc = kb, vc = vb;
         if (b + kw < b1) {
             kb.load_keys(kp + (size_t)(b + kw) * BB, lane);
             vb.load_values(vp + (size_t)(b + kw) * BB, lane);
         }
-        const bool full = (b + 1) * PK_BLOCK <= least;
-        const int key0 = b * PK_BLOCK + 4 * g4;  // this lane's keys: key0 + 16 h + e
+        const int key0 = b * PK_BLOCK + 4 * g4;  // this lane's keys: key0 + 16 h + i
         f32x4 s[NT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -337,17 +367,17 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
                         acc[n][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qv[n][x][st], acc[n][st / 2], 0, 0, 0);
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int n = 0; n < NT; ++n) {
                     float v = 0.f;
 #pragma unroll
                     for (int g = 0; g < GS; ++g) {
                         const uint32_t u = kc.param(h, i, g);
                         const float sk = __uint_as_float(u << 16), mk = __uint_as_float(u & 0xffff0000u);
-                        v += sk * acc[n][g][i] + (CENTRED ? mk - OFF * sk : mk) * qsum[n][g];
+                        v = fmaf(CENTRED ? mk - OFF * sk : mk, qsum[n][g], fmaf(sk, acc[n][g][i], v));
                     }
-                    s[n][h][i] = full || key0 + 16 * h + i < limit[n] ? v : -INFINITY;
+                    s[n][h][i] = MASKED && key0 + 16 * h + i >= limit[n] ? -INFINITY : v;
                 }
         }
         // the columns' probabilities, in place
@@ -374,7 +404,7 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(s[n][h][i] * sc - mu);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n][h][i], sc, -mu));
                     s[n][h][i] = p;
                     l[n] += p;
                 }
@@ -382,22 +412,23 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
             bf16x8 pb[NT][PP];
+            float v[NT][8];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float v[8];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t u = vc.param(h, i, g);
+                    const float sv = __uint_as_float(u << 16), mv = fmaf(-OFF, sv, __uint_as_float(u & 0xffff0000u));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t u = vc.param(h, i, g);
-                        const float sv = __uint_as_float(u << 16), p = s[n][h][i];
+                    for (int n = 0; n < NT; ++n) {
                         // slots that a column does not see may hold anything, a scale of NaN too
-                        const bool seen = full || key0 + 16 * h + i < limit[n];
-                        v[4 * h + i] = seen ? p * sv : 0.f;
-                        z[n][g] += seen ? p * (__uint_as_float(u & 0xffff0000u) - OFF * sv) : 0.f;
+                        const bool hide = MASKED && key0 + 16 * h + i >= limit[n];
+                        v[n][4 * h + i] = s[n][h][i] * (hide ? 0.f : sv);
+                        z[n][g] = fmaf(s[n][h][i], hide ? 0.f : mv, z[n][g]);
                     }
-                pk_pieces<PP>(v, pb[n]);
-            }
+                }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) pk_pieces<PP>(v[n], pb[n]);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {  // 16-dimension tiles of the group
                 const int d = 4 * g + q;
@@ -411,7 +442,12 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
                         o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n][x], o[n][d], 0, 0, 0);
             }
         }
-    }
+    };
+    int b = b0;
+#pragma unroll 1
+    for (; b < b_full; b += kw) step(b, std::false_type{});
+#pragma unroll 1
+    for (; b < b1; b += kw) step(b, std::true_type{});
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] = pk_sum4(l[n]);
