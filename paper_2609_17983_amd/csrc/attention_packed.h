@@ -27,14 +27,22 @@
 // and its probabilities are the second product's operand as they stand.  The packed
 // layout holds the codes in the order of that operand: every load of the key loop is
 // one contiguous piece per wavefront, straight into registers, and no LDS or barrier
-// is in the loop.  Softmax runs in the exp2 domain; a column's running maximum is
-// raised only when a score exceeds it by 2^8, so the cross-lane maximum is rare, and
-// the sums are reduced once, at the end.
+// is in the loop.  A block's keys are loaded again as soon as the scores have used
+// them, its values after the output product.  Softmax runs in the exp2 domain; a
+// column's running maximum is raised only when a score exceeds it by 2^8, so the
+// cross-lane maximum is rare, and the sums are reduced once, at the end.
 //
-// A block of four wavefronts takes (document, column group, kv head, key range):
-// cw wavefronts hold nt 16-column tiles each, and the 4 / cw wavefronts of a tile
-// take alternate 32-key blocks and merge their states through LDS.  Key ranges that
-// are split over blocks leave partials (O, m, l) that a combine kernel joins.
+// Few columns (the next token of a document has G) leave a tile's lanes idle in the
+// softmax, whose work is the larger part.  With at most 16 / CL columns the tile
+// holds them CL times, and of CL key tiles each copy takes one: the scores of a lane
+// are those of its copy's keys, and in the operand of the output product a copy's
+// probabilities are zero for the other tiles' keys.  The copies are columns of their
+// own, with their own maximum and sum, and are joined at the end.
+//
+// A block of threads takes (document, column group, kv head, key range): cw
+// wavefronts hold nt 16-column tiles each, and the wavefronts of a tile take
+// alternate key blocks and join their states through LDS.  Key ranges that are split
+// over blocks of threads leave partials (O, m, l) that a combine kernel joins.
 #include <math.h>
 
 #include <type_traits>
@@ -66,6 +74,13 @@ __device__ __forceinline__ float pk_sum4(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// v of the lane N further on in the 16 lanes of a row (with CL copies of 16 / CL
+// columns: of the same column in another copy).
+template <int N>
+__device__ __forceinline__ float pk_ror(float v) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x120 + N, 0xf, 0xf, true));
+}
+
 // Weight of a partial state with maximum m in one with maximum `all`.  A state
 // without a maximum is empty (zeros) or saw scores of NaN only, which stay.
 __device__ __forceinline__ float pk_weight(float m, float all) {
@@ -75,24 +90,11 @@ __device__ __forceinline__ float pk_weight(float m, float all) {
 // One 32-key block of a plane as a lane loads it.
 template <int HP, int BITS>
 struct PackedBlock {
-    static constexpr int KS = HP / 32, GS = HP / PK_GROUP;
     static constexpr int W = HP * BITS / 256;  // 16-byte units of a lane's codes: 1 (64 wide, 4 bits) .. 4
     static_assert(64 * W * 16 == pk_code_bytes(HP, BITS), "a lane's share of a block");
     u32x4 codes[W];
-    u32x4 par[2][GS];  // scale and offset words of positions 16h + 4g .. +3, groups side by side
     // keys: [16-position tile][KS * BITS / 4 words]; values: [KS * BITS / 2 words]
     __device__ __forceinline__ uint32_t word(int i) const { return codes[i >> 2][i & 3]; }
-    __device__ __forceinline__ uint32_t param(int h, int e, int g) const {
-        const int i = e * GS + g;
-        return par[h][i >> 2][i & 3];
-    }
-    __device__ __forceinline__ void load_params(const char *b, int g4) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < GS; ++i)
-                par[h][i] = *reinterpret_cast<const u32x4 *>(b + pk_code_bytes(HP, BITS) + ((16 * h + 4 * g4) * GS + 4 * i) * 4);
-    }
     __device__ __forceinline__ void load_keys(const char *b, int lane) {
         constexpr int TB = pk_code_bytes(HP, BITS) / 2;  // bytes of a 16-position tile
         if constexpr (W == 1) {
@@ -109,14 +111,26 @@ struct PackedBlock {
                 for (int i = 0; i < W / 2; ++i)
                     codes[h * (W / 2) + i] = *reinterpret_cast<const u32x4 *>(b + h * TB + (lane * (W / 2) + i) * 16);
         }
-        load_params(b, lane >> 4);
     }
     __device__ __forceinline__ void load_values(const char *b, int lane) {
 #pragma unroll
         for (int i = 0; i < W; ++i) codes[i] = *reinterpret_cast<const u32x4 *>(b + (lane * W + i) * 16);
-        load_params(b, lane >> 4);
     }
 };
+
+// Scale and offset words of positions 16 half + 4 g4 .. +3 of a block, groups side by
+// side.
+template <int HP, int BITS>
+__device__ __forceinline__ void pk_params(u32x4 par[HP / PK_GROUP], const char *plane, int b, int half, int g4) {
+    constexpr int GS = HP / PK_GROUP;
+    const char *p = plane + (size_t)b * pk_block_bytes(HP, BITS) + pk_code_bytes(HP, BITS) + (16 * half + 4 * g4) * GS * 4;
+#pragma unroll
+    for (int i = 0; i < GS; ++i) par[i] = reinterpret_cast<const u32x4 *>(p)[i];
+}
+template <int GS>
+__device__ __forceinline__ uint32_t pk_param(const u32x4 par[GS], int i, int g) {
+    return par[(i * GS + g) >> 2][(i * GS + g) & 3];
+}
 
 __device__ __forceinline__ bf16x8 pk_operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d});
@@ -129,16 +143,22 @@ __device__ __forceinline__ bf16x8 pk_bytes(uint32_t a, uint32_t b) {
     return pk_operand(pk_pair((float)(a & 0xffu), (float)((a >> 8) & 0xffu)), pk_pair((float)((a >> 16) & 0xffu), (float)(a >> 24)),
                       pk_pair((float)(b & 0xffu), (float)((b >> 8) & 0xffu)), pk_pair((float)((b >> 16) & 0xffu), (float)(b >> 24)));
 }
+// (x & mask) | bits in one instruction (the compiler makes two of it, with literals).
+__device__ __forceinline__ uint32_t pk_and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(bits));
+    return r;
+}
 // 16 + code for the eight dimensions of a key word.
 __device__ __forceinline__ bf16x8 pk_key4(uint32_t w) {
     constexpr uint32_t M = 0x00780078u, B = 0x41804180u;
-    return pk_operand(((w << 3) & M) | B, ((w >> 1) & M) | B, ((w >> 5) & M) | B, ((w >> 9) & M) | B);
+    return pk_operand(pk_and_or(w << 3, M, B), pk_and_or(w >> 1, M, B), pk_and_or(w >> 5, M, B), pk_and_or(w >> 9, M, B));
 }
 // 16 + code for the four positions each of two value words, of their low (nib 0) or
 // high dimension.
 __device__ __forceinline__ bf16x8 pk_value4(uint32_t a, uint32_t b, int nib) {
     constexpr uint32_t M = 0x78787878u, B = 0x80808080u, X = 0x41414141u;
-    const uint32_t x = ((nib ? a >> 1 : a << 3) & M) | B, y = ((nib ? b >> 1 : b << 3) & M) | B;
+    const uint32_t x = pk_and_or(nib ? a >> 1 : a << 3, M, B), y = pk_and_or(nib ? b >> 1 : b << 3, M, B);
     return pk_operand(__builtin_amdgcn_perm(X, x, 0x04010400u), __builtin_amdgcn_perm(X, x, 0x04030402u),
                       __builtin_amdgcn_perm(X, y, 0x04010400u), __builtin_amdgcn_perm(X, y, 0x04030402u));
 }
@@ -170,6 +190,20 @@ __device__ __forceinline__ void pk_pieces(const float v[8], bf16x8 p[NP]) {
     for (int x = 0; x < NP; ++x) p[x] = __builtin_bit_cast(bf16x8, u[x]);
 }
 
+template <int NP>
+__device__ __forceinline__ void pk_pieces4(const float v[4], uint32_t p[NP][2]) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        f32x2 f = {v[2 * q], v[2 * q + 1]};
+#pragma unroll
+        for (int x = 0; x < NP; ++x) {
+            const bf16x2 h = __builtin_convertvector(f, bf16x2);
+            p[x][q] = __builtin_bit_cast(uint32_t, h);
+            if (x + 1 < NP) f -= __builtin_convertvector(h, f32x2);
+        }
+    }
+}
+
 // n <= 4 values at columns c.. of row r.
 template <typename T>
 __device__ __forceinline__ void pk_store(const PackedAttnArgs &a, int64_t r, int c, int n, bool vec, f32x4 y) {
@@ -196,37 +230,54 @@ __device__ __forceinline__ void pk_store(const PackedAttnArgs &a, int64_t r, int
         store_operand(o, lo, a.o_perm ? perm_offset((int)r, c + e, (int)a.out_stride) : off + e, y[e]);
 }
 
-// T: the model's type.  QP: bf16 pieces of a query; NT: column tiles of a wavefront.
-template <typename T, int HP, int BITS, int QP, int NT>
-__global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(PackedTable t, PackedAttnArgs a, int cw,
-                                                                               int q_vec, int o_vec) {
+// T: the model's type.  QP: bf16 pieces of a query; NT: column tiles of a wavefront;
+// CL: copies of the columns in a tile.
+template <typename T, int HP, int BITS, int QP, int NT, int CL>
+__global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedTable t, PackedAttnArgs a, int cw,
+                                                                            int q_vec, int o_vec) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16;
     constexpr int PP = sizeof(T) == 4 ? 3 : 2;  // bf16 pieces of a probability times a scale
     constexpr bool CENTRED = sizeof(T) == 4;
-    constexpr float RAW = BITS == 4 ? 16.f : 0.f;                              // a loaded code's offset
+    constexpr float RAW = BITS == 4 ? 16.f : 0.f;                      // a loaded code's offset
     constexpr float OFF = !CENTRED ? RAW : BITS == 4 ? -8.f : -128.f;  // the operand's
     constexpr int BB = pk_block_bytes(HP, BITS);
     constexpr int ST = DT * 4 + 2;  // a lane's state per tile: O, m, l
+    // a step takes SB blocks of keys: TT key tiles, H of them for each copy
+    constexpr int SB = CL == 4 ? 2 : 1, TT = 2 * SB, H = TT / CL, CC = 16 / CL;
+    static_assert(CL == 1 || NT == 1, "copies fill one tile");
     extern __shared__ float merge[];
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int copy = (lane & 15) / CC, col = (lane & 15) % CC;
     const int kvh = blockIdx.y;
     const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.x) * PK_ENTRY;
     const int nsplit = e[PKE_SPLITS], item = blockIdx.x - (int)e[PKE_ITEM0];
-    const int cols = 16 * NT * cw;
-    const int kw = PK_ATT_WAVES / cw, wk = w / cw, wc = w - wk * cw;
+    const int cols = CC * NT * cw;
+    const int kw = (int)(blockDim.x >> 6) / cw, wk = w / cw, wc = w - wk * cw;
     const int split = nsplit == 1 ? 0 : item % nsplit;
-    // the first key block's loads wait for nothing else
+    // the first blocks' loads wait for nothing else
     const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
     const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
     const char *vp = kp + a.Hkv * plane;
-    const int b0 = split * (a.range / PK_BLOCK) + wk;
-    PackedBlock<HP, BITS> kb, vb;
-    {
-        const size_t first = (size_t)min(b0, (int)e[PKE_BLOCKS] - 1) * BB;
-        kb.load_keys(kp + first, lane);
-        vb.load_values(vp + first, lane);
-    }
+    const int last = (int)e[PKE_BLOCKS] - 1;
+    PackedBlock<HP, BITS> kb[SB], vb[SB];
+    u32x4 kpar[H][GS], vpar[H][GS];  // of this lane's keys
+    // Blocks b .. b + SB - 1; an odd document's last step loads its last block twice.
+    auto load_keys = [&](int b) {
+#pragma unroll
+        for (int x = 0; x < SB; ++x) kb[x].load_keys(kp + (size_t)min(b + x, last) * BB, lane);
+#pragma unroll
+        for (int h = 0; h < H; ++h) pk_params<HP, BITS>(kpar[h], kp, min(b + (h * CL + copy) / 2, last), (h * CL + copy) & 1, g4);
+    };
+    auto load_values = [&](int b) {
+#pragma unroll
+        for (int x = 0; x < SB; ++x) vb[x].load_values(vp + (size_t)min(b + x, last) * BB, lane);
+#pragma unroll
+        for (int h = 0; h < H; ++h) pk_params<HP, BITS>(vpar[h], vp, min(b + (h * CL + copy) / 2, last), (h * CL + copy) & 1, g4);
+    };
+    const int b0 = split * (a.range / PK_BLOCK) + wk * SB;
+    load_keys(min(b0, last));
+    load_values(min(b0, last));
     const int G = a.Hq / a.Hkv, ncols_doc = (int)e[PKE_ROWS] * G;
     // column groups from the last one down: later rows see more keys
     const int ncg = (ncols_doc + cols - 1) / cols;
@@ -240,7 +291,7 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
     int top = 0, least = 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int c = cg * cols + (wc * NT + n) * 16 + (lane & 15);
+        const int c = cg * cols + (wc * NT + n) * CC + col;
         const bool valid = c < ncols_doc;
         row[n] = valid ? c / G : 0;
         head[n] = kvh * G + (valid ? c - row[n] * G : 0);
@@ -313,14 +364,15 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
     }
     // the wavefront's last visible key, and the keys that all its columns see
 #pragma unroll
-    for (int o = 1; o < 16; o *= 2) {
+    for (int o = 1; o < CC; o *= 2) {
         top = max(top, __shfl_xor(top, o, 64));
         least = min(least, __shfl_xor(least, o, 64));
     }
     top = __builtin_amdgcn_readfirstlane(top);
     least = __builtin_amdgcn_readfirstlane(least);
     const int b1 = (min(top, (split + 1) * a.range) + PK_BLOCK - 1) / PK_BLOCK;
-    const int b_full = min(b1, least / PK_BLOCK);  // blocks before it need no mask
+    // steps that begin before it need no mask
+    const int b_full = min(b1, least / PK_BLOCK) - (SB - 1);
 
     f32x4 o[NT][DT];
     float m[NT], l[NT], z[NT][GS];
@@ -334,37 +386,48 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
         l[n] = 0.f;
     }
     const float sc = 1.4426950408889634f / sqrtf((float)a.hd);
+    uint32_t mine[CL];  // all ones for this lane's copy
+#pragma unroll
+    for (int c = 0; c < CL; ++c) mine[c] = copy == c ? 0xffffffffu : 0u;
 
-    // one block of keys; masked: a column may not see all of them
+    // one step; masked: a column may not see all of its keys
     auto step = [&](int b, auto masked_) {
         constexpr bool MASKED = decltype(masked_)::value;
-        const PackedBlock<HP, BITS> kc = kb, vc = vb;
-        if (b + kw < b1) {
-            kb.load_keys(kp + (size_t)(b + kw) * BB, lane);
-            vb.load_values(vp + (size_t)(b + kw) * BB, lane);
-        }
-        const int key0 = b * PK_BLOCK + 4 * g4;  // this lane's keys: key0 + 16 h + i
-        f32x4 s[NT][2];
+        const bool more = b + kw * SB < b1;
+        const int key0 = b * PK_BLOCK + 16 * copy + 4 * g4;  // this lane's keys: key0 + 16 CL h + i
+        f32x4 s[NT][H];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
             f32x4 acc[NT][GS];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int g = 0; g < GS; ++g) {
-                    const float i = CENTRED ? 0.f : -OFF * qsum[n][g];
-                    acc[n][g] = f32x4{i, i, i, i};
-                }
-#pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                bf16x8 ka = BITS == 4 ? pk_key4(kc.word(h * KS + st))
-                                      : pk_bytes(kc.word((h * KS + st) * 2), kc.word((h * KS + st) * 2 + 1));
-                if (CENTRED) ka = pk_less(ka, RAW - OFF);
+            for (int c = 0; c < CL; ++c) {
+                const int tile = h * CL + c;
+                f32x4 one[NT][GS];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int x = 0; x < QP; ++x)
-                        acc[n][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qv[n][x][st], acc[n][st / 2], 0, 0, 0);
+                    for (int g = 0; g < GS; ++g) {
+                        const float i = CENTRED ? 0.f : -OFF * qsum[n][g];
+                        one[n][g] = f32x4{i, i, i, i};
+                    }
+#pragma unroll
+                for (int st = 0; st < KS; ++st) {
+                    const PackedBlock<HP, BITS> &k = kb[tile >> 1];
+                    const int i = (tile & 1) * KS + st;
+                    bf16x8 ka = BITS == 4 ? pk_key4(k.word(i)) : pk_bytes(k.word(2 * i), k.word(2 * i + 1));
+                    if (CENTRED) ka = pk_less(ka, RAW - OFF);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int x = 0; x < QP; ++x)
+                            one[n][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qv[n][x][st], one[n][st / 2], 0, 0, 0);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int g = 0; g < GS; ++g)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[n][g][i] = c == 0 || copy == c ? one[n][g][i] : acc[n][g][i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -373,19 +436,20 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
                     float v = 0.f;
 #pragma unroll
                     for (int g = 0; g < GS; ++g) {
-                        const uint32_t u = kc.param(h, i, g);
+                        const uint32_t u = pk_param<GS>(kpar[h], i, g);
                         const float sk = __uint_as_float(u << 16), mk = __uint_as_float(u & 0xffff0000u);
                         v = fmaf(CENTRED ? mk - OFF * sk : mk, qsum[n][g], fmaf(sk, acc[n][g][i], v));
                     }
-                    s[n][h][i] = MASKED && key0 + 16 * h + i >= limit[n] ? -INFINITY : v;
+                    s[n][h][i] = MASKED && key0 + 16 * CL * h + i >= limit[n] ? -INFINITY : v;
                 }
         }
+        if (more) load_keys(b + kw * SB);
         // the columns' probabilities, in place
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float mx = -INFINITY;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][h][i]);
             mx *= sc;
@@ -401,7 +465,7 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
             }
             const float mu = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float p = __builtin_amdgcn_exp2f(fmaf(s[n][h][i], sc, -mu));
@@ -411,43 +475,68 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
         }
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
-            bf16x8 pb[NT][PP];
-            float v[NT][8];
+            uint32_t pw[NT][H][PP][2];  // the pieces of four probabilities times scales
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < H; ++h) {
+                float sv[4], mv[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t u = vc.param(h, i, g);
-                    const float sv = __uint_as_float(u << 16), mv = fmaf(-OFF, sv, __uint_as_float(u & 0xffff0000u));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        // slots that a column does not see may hold anything, a scale of NaN too
-                        const bool hide = MASKED && key0 + 16 * h + i >= limit[n];
-                        v[n][4 * h + i] = s[n][h][i] * (hide ? 0.f : sv);
-                        z[n][g] = fmaf(s[n][h][i], hide ? 0.f : mv, z[n][g]);
-                    }
+                    const uint32_t u = pk_param<GS>(vpar[h], i, g);
+                    sv[i] = __uint_as_float(u << 16);
+                    mv[i] = fmaf(-OFF, sv[i], __uint_as_float(u & 0xffff0000u));
                 }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) pk_pieces<PP>(v[n], pb[n]);
+                for (int n = 0; n < NT; ++n) {
+                    float v[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {  // 16-dimension tiles of the group
-                const int d = 4 * g + q;
-                bf16x8 va = BITS == 4 ? pk_value4(vc.word((d >> 1) * 2), vc.word((d >> 1) * 2 + 1), d & 1)
-                                      : pk_bytes(vc.word(d * 2), vc.word(d * 2 + 1));
-                if (CENTRED) va = pk_less(va, RAW - OFF);
+                    for (int i = 0; i < 4; ++i) {
+                        // slots that a column does not see may hold anything, a scale of NaN too
+                        const bool hide = MASKED && key0 + 16 * CL * h + i >= limit[n];
+                        v[i] = s[n][h][i] * (hide ? 0.f : sv[i]);
+                        z[n][g] = fmaf(s[n][h][i], hide ? 0.f : mv[i], z[n][g]);
+                    }
+                    pk_pieces4<PP>(v, pw[n][h]);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < SB; ++x) {
+                // slots 0..3 of the operand are the block's first tile's keys, 4..7 the second's
+                bf16x8 pb[NT][PP];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int x = 0; x < PP; ++x)
-                        o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n][x], o[n][d], 0, 0, 0);
+                    for (int q = 0; q < PP; ++q) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int tile = 2 * x + k / 2;
+                            u[k] = pw[n][tile / CL][q][k & 1];
+                            if (CL > 1) u[k] &= mine[tile % CL];
+                        }
+                        pb[n][q] = pk_operand(u[0], u[1], u[2], u[3]);
+                    }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {  // 16-dimension tiles of the group
+                    const int d = 4 * g + q;
+                    bf16x8 va = BITS == 4 ? pk_value4(vb[x].word((d >> 1) * 2), vb[x].word((d >> 1) * 2 + 1), d & 1)
+                                          : pk_bytes(vb[x].word(d * 2), vb[x].word(d * 2 + 1));
+                    if (CENTRED) va = pk_less(va, RAW - OFF);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int y = 0; y < PP; ++y)
+                            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n][y], o[n][d], 0, 0, 0);
+                }
             }
         }
+        if (more) load_values(b + kw * SB);
     };
     int b = b0;
 #pragma unroll 1
-    for (; b < b_full; b += kw) step(b, std::false_type{});
+    for (; b < b_full; b += kw * SB) step(b, std::false_type{});
 #pragma unroll 1
-    for (; b < b1; b += kw) step(b, std::true_type{});
+    for (; b < b1; b += kw * SB) step(b, std::true_type{});
+
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] = pk_sum4(l[n]);
@@ -457,80 +546,98 @@ __global__ __launch_bounds__(64 * PK_ATT_WAVES, 2) void attention_packed_kernel(
 #pragma unroll
             for (int q = 0; q < 4; ++q) o[n][4 * g + q] += y;
         }
-    }
-    // the wavefronts of a tile, merged into the first one
-    if (kw > 1) {
-        if (wk > 0) {
-            float *p = merge + (size_t)((wk - 1) * cw + wc) * NT * ST * 64 + lane;
+        if constexpr (CL > 1) {  // the copies of a column
+            float all = fmaxf(m[n], pk_ror<CC>(m[n]));
+            if (CL == 4) all = fmaxf(all, pk_ror<8>(all));
+            const float f = pk_weight(m[n], all);
+            m[n] = all;
+            auto join = [&](float v) {
+                v *= f;
+                v += pk_ror<CC>(v);
+                return CL == 4 ? v + pk_ror<8>(v) : v;
+            };
+            l[n] = join(l[n]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[(n * ST + d * 4 + i) * 64] = o[n][d][i];
-                p[(n * ST + DT * 4) * 64] = m[n];
-                p[(n * ST + DT * 4 + 1) * 64] = l[n];
-            }
-        }
-        __syncthreads();
-        if (wk > 0) return;
-#pragma unroll 1
-        for (int k = 1; k < kw; ++k) {
-            const float *p = merge + (size_t)((k - 1) * cw + wc) * NT * ST * 64 + lane;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float m1 = p[(n * ST + DT * 4) * 64], l1 = p[(n * ST + DT * 4 + 1) * 64];
-                const float mn = fmaxf(m[n], m1);
-                const float a0 = pk_weight(m[n], mn), a1 = pk_weight(m1, mn);
-                m[n] = mn;
-                l[n] = l[n] * a0 + l1 * a1;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[n][d][i] = o[n][d][i] * a0 + p[(n * ST + d * 4 + i) * 64] * a1;
-            }
+                for (int i = 0; i < 4; ++i) o[n][d][i] = join(o[n][d][i]);
         }
     }
-    // lane: column lane%16, dimensions 16 d + 4 g4 + i
+    // Lane: one column, dimensions 16 d + 4 g4 + i.  The wavefronts of a tile hand their
+    // states to each other through LDS, and wavefront wk finishes the dimension tiles wk,
+    // wk + kw, ..
+    float *const mg = merge + (size_t)wc * NT * ST * 64 + lane;
+    const int mstep = cw * NT * ST * 64;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        if (row[n] < 0) continue;
-        if (nsplit == 1) {
-            const float inv = l[n] == 0.f ? 0.f : 1.0f / l[n];
+        float *p = mg + wk * mstep + n * ST * 64;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const int c = 16 * d + 4 * g4;
-                if (c < a.hd)
-                    pk_store<T>(a, row0 + row[n], head[n] * a.hd + c, min(4, a.hd - c), o_vec, o[n][d] * inv);
-            }
-        } else {
-            const int c = (wc * NT + n) * 16 + (lane & 15);
-            float *p = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * cols + c) * (HP + 4);
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4 *>(p + 16 * d + 4 * g4) = o[n][d];
-            if (g4 == 0) {
-                p[HP] = m[n];
-                p[HP + 1] = l[n];
-            }
+            for (int i = 0; i < 4; ++i) p[(d * 4 + i) * 64] = o[n][d][i];
+        p[DT * 4 * 64] = m[n];
+        p[(DT * 4 + 1) * 64] = l[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (row[n] < 0 || copy > 0) continue;
+        const float *p = mg + n * ST * 64;
+        float all = -INFINITY, sum = 0.f, f[PK_WAVES_MAX];
+#pragma unroll
+        for (int k = 0; k < PK_WAVES_MAX; ++k) f[k] = k < kw ? p[k * mstep + DT * 4 * 64] : -INFINITY;
+#pragma unroll
+        for (int k = 0; k < PK_WAVES_MAX; ++k) all = fmaxf(all, f[k]);
+#pragma unroll
+        for (int k = 0; k < PK_WAVES_MAX; ++k) {
+            f[k] = pk_weight(f[k], all);
+            if (k < kw) sum += p[k * mstep + (DT * 4 + 1) * 64] * f[k];
+        }
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+        const int c = (wc * NT + n) * CC + col;
+        float *part = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * cols + c) * (HP + 4);
+#pragma unroll 1
+        for (int d = wk; d < DT; d += kw) {
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < PK_WAVES_MAX; ++k)
+                if (k < kw) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] += p[k * mstep + (d * 4 + i) * 64] * f[k];
+                }
+            const int dim = 16 * d + 4 * g4;
+            if (nsplit > 1) *reinterpret_cast<f32x4 *>(part + dim) = y;
+            else if (dim < a.hd) pk_store<T>(a, row0 + row[n], head[n] * a.hd + dim, min(4, a.hd - dim), o_vec, y * inv);
+        }
+        if (nsplit > 1 && g4 == 0 && wk == 0) {
+            part[HP] = all;
+            part[HP + 1] = sum;
         }
     }
 }
 
-template <typename T, int HP, int BITS, int QP, int NT>
-hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, int cw, bool q_vec, bool o_vec, hipStream_t s) {
-    const int kw = PK_ATT_WAVES / cw;
-    const uint32_t lds = (uint32_t)(kw - 1) * cw * NT * (HP / 4 + 2) * 64 * 4;
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, NT>), dim3(a.n_items, a.Hkv), dim3(64 * PK_ATT_WAVES), lds, s, t, a,
-               cw, (int)q_vec, (int)o_vec);
+template <typename T, int HP, int BITS, int QP, int NT, int CL>
+hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s) {
+    const uint32_t lds = (uint32_t)sh.waves * NT * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
+    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, NT, CL>), dim3(a.n_items, a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
+               sh.cw, (int)q_vec, (int)o_vec);
     return hipGetLastError();
+}
+
+template <typename T, int HP, int BITS, int QP>
+hipError_t pk_launch_copies(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec,
+                            hipStream_t s) {
+    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 1, 4>(t, a, sh, q_vec, o_vec, s);
+    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 1, 2>(t, a, sh, q_vec, o_vec, s);
+    return pk_launch<T, HP, BITS, QP, 1, 1>(t, a, sh, q_vec, o_vec, s);
 }
 
 template <int HP, int BITS>
 hipError_t pk_launch_bits(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, bool q_vec, bool o_vec,
                           hipStream_t s) {
-    if (!bf16) return pk_launch<float, HP, BITS, 3, 1>(t, a, sh.cw, q_vec, o_vec, s);
-    return a.q_lo ? pk_launch<bf16_t, HP, BITS, 2, 1>(t, a, sh.cw, q_vec, o_vec, s)
-                  : pk_launch<bf16_t, HP, BITS, 1, 1>(t, a, sh.cw, q_vec, o_vec, s);
+    if (!bf16) return pk_launch_copies<float, HP, BITS, 3>(t, a, sh, q_vec, o_vec, s);
+    return a.q_lo ? pk_launch_copies<bf16_t, HP, BITS, 2>(t, a, sh, q_vec, o_vec, s)
+                  : pk_launch_copies<bf16_t, HP, BITS, 1>(t, a, sh, q_vec, o_vec, s);
 }
 
 template <int HP>

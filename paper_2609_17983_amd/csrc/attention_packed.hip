@@ -8,45 +8,78 @@ namespace kvr {
 
 namespace {
 
-// Joins the partials of a column group's key ranges: a wavefront per column.
-template <typename T, int HP>
+// Joins the partials of a column's key ranges.  HP / 4 lanes read a partial; a column's
+// WC wavefronts take WC * 256 / HP ranges at a time, UN of them in flight, each group
+// keeps a running maximum, and the groups are joined through LDS.
+template <typename T, int HP, int WC>
 __global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedTable t, PackedAttnArgs a, int cols, int o_vec) {
+    constexpr int L = HP / 4, GR = 64 / L, UN = 4;
+    __shared__ float red[4][64][6];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kvh = blockIdx.y;
-    const int tiles = cols / 16, x = blockIdx.x / tiles;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_CG0, x) * PK_ENTRY;
-    const int ns = e[PKE_SPLITS], cg = x - (int)e[PKE_CG0], G = a.Hq / a.Hkv;
-    if (ns <= 1) return;
-    const int ncols = (int)e[PKE_ROWS] * G;
-    for (int k = w; k < 16; k += 4) {
-        const int cc = (blockIdx.x % tiles) * 16 + k, c = cg * cols + cc;
-        if (c >= ncols) return;
+    const int x = blockIdx.x * (4 / WC) + w / WC;  // column of the launch
+    const int cgx = min(x / cols, a.n_cg - 1), cc = x % cols;
+    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_CG0, cgx) * PK_ENTRY;
+    const int G = a.Hq / a.Hkv, c = (cgx - (int)e[PKE_CG0]) * cols + cc;
+    const int ns = x / cols < a.n_cg && c < (int)e[PKE_ROWS] * G ? (int)e[PKE_SPLITS] : 1;
+    // (the same for all wavefronts of a column; with WC > 1 of the block)
+    float m = -INFINITY, l = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    if (ns > 1) {
         const size_t step = (size_t)a.Hkv * cols * (HP + 4);
-        const float *p = a.part + (((size_t)((int)e[PKE_PART0] + cg * ns) * a.Hkv + kvh) * cols + cc) * (HP + 4);
-        // the ranges' maxima and sums, one range a lane
-        float mx = -INFINITY;
-        for (int i = lane; i < ns; i += 64) mx = fmaxf(mx, p[i * step + HP]);
+        const float *p = a.part + (((size_t)((int)e[PKE_PART0] + (cgx - (int)e[PKE_CG0]) * ns) * a.Hkv + kvh) * cols + cc) * (HP + 4);
+        const int d = (lane % L) * 4, first = (w % WC) * GR + lane / L;
+        for (int i0 = first; i0 < ns; i0 += UN * WC * GR) {
+            f32x4 v[UN];
+            float mi[UN], li[UN];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        float l = 0.f;
-        for (int i = lane; i < ns; i += 64) l += p[i * step + HP + 1] * pk_weight(p[i * step + HP], mx);
+            for (int u = 0; u < UN; ++u) {
+                const float *q = p + (size_t)min(i0 + u * WC * GR, ns - 1) * step;
+                v[u] = *reinterpret_cast<const f32x4 *>(q + d);
+                mi[u] = q[HP];
+                li[u] = q[HP + 1];
+            }
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        // the outputs: half a wavefront (64 wide: a quarter) takes every other (fourth) range
-        constexpr int L = HP / 4, PARTS = 64 / L;
-        const int d = (lane % L) * 4, part = lane / L;
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-        for (int i = part; i < ns; i += PARTS)
-            y += *reinterpret_cast<const f32x4 *>(p + i * step + d) * pk_weight(p[i * step + HP], mx);
-#pragma unroll
-        for (int o = 32; o >= L; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] += __shfl_xor(y[i], o, 64);
-        if (part == 0 && d < a.hd) {
-            const int r = c / G, h = kvh * G + c - r * G;
-            pk_store<T>(a, (int64_t)e[PKE_ROW0] + r, h * a.hd + d, min(4, a.hd - d), o_vec, y * inv);
+            for (int u = 0; u < UN; ++u) {
+                if (i0 + u * WC * GR >= ns) continue;
+                const float all = fmaxf(m, mi[u]), f0 = pk_weight(m, all), f1 = pk_weight(mi[u], all);
+                m = all;
+                l = l * f0 + li[u] * f1;
+                y = y * f0 + v[u] * f1;
+            }
         }
     }
+    // the groups of lanes, then the wavefronts
+#pragma unroll
+    for (int o = L; o < 64; o *= 2) {
+        const float m1 = __shfl_xor(m, o, 64), l1 = __shfl_xor(l, o, 64), all = fmaxf(m, m1);
+        const float f0 = pk_weight(m, all), f1 = pk_weight(m1, all);
+        m = all;
+        l = l * f0 + l1 * f1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = y[i] * f0 + __shfl_xor(y[i], o, 64) * f1;
+    }
+    if constexpr (WC > 1) {
+        float *r = red[w][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = y[i];
+        r[4] = m;
+        r[5] = l;
+        __syncthreads();
+        if (w > 0) return;
+#pragma unroll
+        for (int k = 1; k < WC; ++k) {
+            const float *q = red[k][lane];
+            const float all = fmaxf(m, q[4]), f0 = pk_weight(m, all), f1 = pk_weight(q[4], all);
+            m = all;
+            l = l * f0 + q[5] * f1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = y[i] * f0 + q[i] * f1;
+        }
+    }
+    const int d = (lane % L) * 4;
+    if (ns <= 1 || lane >= L || d >= a.hd) return;
+    const int r = c / G, h = kvh * G + c - r * G;
+    pk_store<T>(a, (int64_t)e[PKE_ROW0] + r, h * a.hd + d, min(4, a.hd - d), o_vec, y * (l == 0.f ? 0.f : 1.0f / l));
 }
 
 }  // namespace
@@ -57,8 +90,10 @@ hipError_t launch_attention_packed64(bool bf16, int bits, PackedShape sh, const 
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                    hipStream_t s) {
     if (a.n_items <= 0) return hipSuccess;
-    if (a.hd > 128 || (bits != 4 && bits != 8) || a.n_docs > PK_MAX_DOCS || sh.nt != 1 ||
-        (sh.cw != 1 && sh.cw != 2 && sh.cw != 4) || a.range % PK_BLOCK != 0)
+    // (a step is two blocks where a tile holds four copies)
+    if (a.hd > 128 || (bits != 4 && bits != 8) || a.n_docs > PK_MAX_DOCS || sh.nt != 1 || sh.cw < 1 || sh.waves % sh.cw != 0 ||
+        sh.waves > PK_WAVES_MAX || (sh.copies != 1 && sh.copies != 2 && sh.copies != 4) ||
+        a.range % (PK_BLOCK * (sh.copies == 4 ? 2 : 1)) != 0)
         return hipErrorInvalidValue;
     return pk_width(a.hd) == 64 ? launch_attention_packed64(bf16, bits, sh, t, a, s)
                                 : pk_launch_width<128>(bf16, bits, sh, t, a, s);
@@ -67,17 +102,24 @@ hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const Pa
 hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                            hipStream_t s) {
     const int cols = pk_cols(sh);
-    const dim3 grid(a.n_cg * (cols / 16), a.Hkv);
     const size_t es = bf16 ? 2 : 4;
     const int o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * es - 1)) == 0 &&
                       ((uintptr_t)a.out_lo & (4 * es - 1)) == 0;
+    const int wc = a.max_splits > 8 ? 4 : 1;
+    const dim3 grid((unsigned)(((size_t)a.n_cg * cols * wc + 3) / 4), a.Hkv);
+#define KVR_COMBINE(T, HP)                                                                                                    \
+    do {                                                                                                                      \
+        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, t, a, cols, o_vec);       \
+        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, t, a, cols, o_vec);               \
+    } while (0)
     if (pk_width(a.hd) == 64) {
-        if (bf16) kvr_launch((attention_packed_combine_kernel<bf16_t, 64>), grid, dim3(256), 0, s, t, a, cols, o_vec);
-        else kvr_launch((attention_packed_combine_kernel<float, 64>), grid, dim3(256), 0, s, t, a, cols, o_vec);
+        if (bf16) KVR_COMBINE(bf16_t, 64);
+        else KVR_COMBINE(float, 64);
     } else {
-        if (bf16) kvr_launch((attention_packed_combine_kernel<bf16_t, 128>), grid, dim3(256), 0, s, t, a, cols, o_vec);
-        else kvr_launch((attention_packed_combine_kernel<float, 128>), grid, dim3(256), 0, s, t, a, cols, o_vec);
+        if (bf16) KVR_COMBINE(bf16_t, 128);
+        else KVR_COMBINE(float, 128);
     }
+#undef KVR_COMBINE
     return hipGetLastError();
 }
 

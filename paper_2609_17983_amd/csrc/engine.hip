@@ -47,10 +47,10 @@ struct Tables {
     struct PackedLaunch {
         PackedTable table;
         int n_docs, n_items, n_cg;
-        bool combine;
+        int splits;  // largest number of key ranges
     };
     std::vector<PackedLaunch> packed;
-    PackedShape packed_shape{1, 1};
+    PackedShape packed_shape{};
     int packed_range = 0;
     int att_mt = 1;  // 16-row tiles per attention item (rows of a row block / 16)
     void clear() {
@@ -624,8 +624,10 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
     int most = 0;
     for (int i = 0; i < n_docs; ++i) most = std::max(most, doc(i).n);
     const long long most_cols = (long long)most * G;
-    const PackedShape sh = {1, most_cols <= 16 ? 1 : most_cols <= 32 ? 2 : 4};
-    const int cols = pk_cols(sh), kw = PK_ATT_WAVES / sh.cw;
+    PackedShape sh{1, 1, 1, 4};
+    if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
+    else sh.cw = most_cols <= 32 ? 2 : 4;
+    const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
     long long items = 0, units = 0;
     int longest = 0;
     for (int i = 0; i < n_docs; ++i) {
@@ -637,10 +639,21 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
         units += ncg * Hkv * pk_blocks(keys);
         longest = std::max(longest, keys);
     }
-    // About three blocks to a compute unit; every wavefront has at least two of
-    // the 32-key steps.
+    // Key ranges (measured in us a call; 256 units hold two wavefronts per SIMD):
+    // - much work for few columns, bound by memory: blocks of four wavefronts, about three
+    //   to a unit, so that units that finish early take more (64 documents of 2000-8000
+    //   positions: 85; one block per document 88, blocks of eight 90-94);
+    // - little work: blocks of eight wavefronts, one to a unit, two steps a wavefront at
+    //   least (one document of 40001 positions 18, 768 blocks 24; 48 rows 17 and 24);
+    // - many columns, whose partials cost more than an uneven end: not split once there
+    //   is a block for every unit (1237 rows: 43, split 66-80).
+    const int steps = 4 * sb;
+    const bool large = most_cols <= 16 && units >= 6ll * 768 * steps;
+    sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
+    const int kw = sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
     long long range = pk_blocks(std::max(longest, 1));
-    if (items < 768) range = std::min(range, std::max<long long>(2 * kw, (units + 767) / 768));
+    if (large || items < 256) range = std::min(range, std::max<long long>(2 * kw * sb, (units + target - 1) / target));
+    range = (range + sb - 1) / sb * sb;
     const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
     while (range < pk_blocks(longest) && (pk_blocks(longest) + range - 1) / range * per_row > slots) range *= 2;
@@ -654,7 +667,7 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
         out.emplace_back();
         Tables::PackedLaunch &l = out.back();
         l.n_docs = l.n_items = l.n_cg = 0;
-        l.combine = false;
+        l.splits = 1;
         fill = TableFill(&l.table);
         used = 0;
     };
@@ -684,10 +697,8 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
             l.n_docs = fill.docs;
             l.n_items += ncg * ns;
             l.n_cg += ncg;
-            if (ns > 1) {
-                l.combine = true;
-                used += ncg * ns;
-            }
+            l.splits = std::max(l.splits, ns);
+            if (ns > 1) used += ncg * ns;
             q.row0 += n;
             q.pos += (size_t)n * q.step;
             q.n -= n;
@@ -705,6 +716,7 @@ PackedAttnArgs packed_args(const kvr_ctx *c, const Tables &t, const Tables::Pack
     a.n_items = l.n_items;
     a.n_cg = l.n_cg;
     a.range = t.packed_range;
+    a.max_splits = l.splits;
     return a;
 }
 
@@ -880,7 +892,7 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
         for (const auto &pl : t.packed) {  // packed caches only
             KVR_CHECK(launch_attention_packed(bf, bits, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
                       "attention_packed", ST_ATTN);
-            if (pl.combine)
+            if (pl.splits > 1)
                 KVR_CHECK(launch_attention_packed_combine(bf, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
                           "attention_packed_combine", ST_COMBINE);
         }
@@ -1871,7 +1883,7 @@ static kvr_status attention_packed(kvr_ctx *c, int32_t layer, int32_t bits, cons
     a.layer = layer;
     for (const auto &l : t.packed) {
         hipError_t e = launch_attention_packed(c->bf16, bits, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
-        if (e == hipSuccess && l.combine)
+        if (e == hipSuccess && l.splits > 1)
             e = launch_attention_packed_combine(c->bf16, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(c, e, "kvr_attention_packed");
     }

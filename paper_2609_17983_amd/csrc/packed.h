@@ -109,14 +109,15 @@ struct PackedAttnArgs {
     float *part;
     int32_t layer, Hq, Hkv, hd;
     int32_t n_docs, n_items, n_cg;
-    int32_t range;          // keys of a key range (a multiple of PK_BLOCK)
+    int32_t range;          // keys of a key range (a multiple of a step's)
+    int32_t max_splits;     // largest number of key ranges of a document
 };
-// Columns (row, query head of the kv head's group) of a column group: nt 16-column
-// tiles for each of cw wavefronts; the block's 4 / cw wavefronts of a tile take
-// alternate key blocks.
-struct PackedShape { int nt, cw; };
-constexpr int pk_cols(PackedShape s) { return 16 * s.nt * s.cw; }
-constexpr int PK_ATT_WAVES = 4;
+// A block of `waves` wavefronts: cw of them hold nt column tiles each, with the
+// columns (row, query head of the kv head's group) `copies` times in a tile; the
+// waves / cw wavefronts of a tile take alternate key blocks.
+struct PackedShape { int nt, cw, copies, waves; };
+constexpr int pk_cols(PackedShape s) { return 16 / s.copies * s.nt * s.cw; }
+constexpr int PK_WAVES_MAX = 8;
 constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                    hipStream_t s);
