@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(os.path.dirname(PKG), "_build")
 LIB = os.path.join(PKG, "libkvr.so")
 
-SOURCES = ["engine.hip", "kernels_basic.hip", "gemm_skinny.hip", "gemm_tiled.hip", "gemm_tall.hip", "gemm_generic.hip", "attention.hip", "attention64.hip", "attention_generic.hip", "attention_packed.hip", "attention_packed64.hip",
+SOURCES = ["engine.hip", "kernels_basic.hip", "gemm_skinny.hip", "gemm_tiled.hip", "gemm_tall.hip", "gemm_generic.hip", "attention.hip", "attention64.hip", "attention_generic.hip", "attention_packed.hip", "attention_packed64.hip", "attention_packed_rows.hip",
            "packed.hip", "pack.hip",
            "scoring.hip", "select_gpu.hip", "select.cpp", "metrics.cpp"]
 

@@ -40,9 +40,11 @@
 // own, with their own maximum and sum, and are joined at the end.
 //
 // A block of threads takes (document, column group, kv head, key range): cw
-// wavefronts hold nt 16-column tiles each, and the wavefronts of a tile take
-// alternate key blocks and join their states through LDS.  Key ranges that are split
-// over blocks of threads leave partials (O, m, l) that a combine kernel joins.
+// wavefronts hold a 16-column tile each, and the wavefronts of a tile take alternate
+// key blocks and join their states through LDS.  Key ranges that are split over
+// blocks of threads leave partials (O, m, l) that a combine kernel joins.
+//
+// bf16 models with many columns take attention_packed_rows.hip instead.
 #include <math.h>
 
 #include <type_traits>
@@ -230,9 +232,77 @@ __device__ __forceinline__ void pk_store(const PackedAttnArgs &a, int64_t r, int
         store_operand(o, lo, a.o_perm ? perm_offset((int)r, c + e, (int)a.out_stride) : off + e, y[e]);
 }
 
-// T: the model's type.  QP: bf16 pieces of a query; NT: column tiles of a wavefront;
-// CL: copies of the columns in a tile.
-template <typename T, int HP, int BITS, int QP, int NT, int CL>
+// A lane's part of the query operand: dimensions 32 s + 8 g4 .. +8 of one row and head
+// (zeros behind hd), as QP bf16 pieces, and their sums by group.
+template <typename T, int HP, int QP>
+__device__ __forceinline__ void pk_query(const PackedAttnArgs &a, int64_t row, int head, int g4, int q_vec,
+                                         bf16x8 qv[QP][HP / 32], float qsum[HP / PK_GROUP]) {
+    constexpr int KS = HP / 32;
+    const size_t q0 = (size_t)(row * a.q_stride) + head * a.hd;
+    const T *q = (const T *)a.q + q0;
+#pragma unroll
+    for (int g = 0; g < HP / PK_GROUP; ++g) qsum[g] = 0.f;
+    if constexpr (QP <= 2) {
+        u32x4 u[QP][KS];
+        if (q_vec) {  // hd is a multiple of 8
+#pragma unroll
+            for (int x = 0; x < QP; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    u[x][s] = *reinterpret_cast<const u32x4 *>((x ? (const T *)a.q_lo + q0 : q) + min(32 * s + 8 * g4, a.hd - 8));
+#pragma unroll
+            for (int x = 0; x < QP; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    if (32 * s + 8 * g4 >= a.hd) u[x][s] = u32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int x = 0; x < QP; ++x)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    u[x][s] = u32x4{0, 0, 0, 0};
+                    for (int j = 0; j < 8; ++j) {
+                        const int d = 32 * s + 8 * g4 + j;
+                        const uint32_t v = d < a.hd ? (uint32_t)(x ? (const T *)a.q_lo + q0 : q)[d] : 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k == j >> 1) u[x][s][k] |= v << (16 * (j & 1));
+                    }
+                }
+        }
+#pragma unroll
+        for (int x = 0; x < QP; ++x)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                qv[x][s] = __builtin_bit_cast(bf16x8, u[x][s]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    qsum[s / 2] += __uint_as_float(u[x][s][j] << 16) + __uint_as_float(u[x][s][j] & 0xffff0000u);
+            }
+    } else {
+        float v[KS][8];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[s][j] = (float)q[min(32 * s + 8 * g4 + j, a.hd - 1)];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (32 * s + 8 * g4 + j >= a.hd) v[s][j] = 0.f;
+                qsum[s / 2] += v[s][j];
+            }
+            bf16x8 p[QP];
+            pk_pieces<QP>(v[s], p);
+#pragma unroll
+            for (int x = 0; x < QP; ++x) qv[x][s] = p[x];
+        }
+    }
+}
+
+// T: the model's type.  QP: bf16 pieces of a query; CL: copies of the columns in a
+// tile.
+template <typename T, int HP, int BITS, int QP, int CL>
 __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedTable t, PackedAttnArgs a, int cw,
                                                                             int q_vec, int o_vec) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16;
@@ -244,7 +314,6 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     constexpr int ST = DT * 4 + 2;  // a lane's state per tile: O, m, l
     // a step takes SB blocks of keys: TT key tiles, H of them for each copy
     constexpr int SB = CL == 4 ? 2 : 1, TT = 2 * SB, H = TT / CL, CC = 16 / CL;
-    static_assert(CL == 1 || NT == 1, "copies fill one tile");
     extern __shared__ float merge[];
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -252,7 +321,7 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     const int kvh = blockIdx.y;
     const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.x) * PK_ENTRY;
     const int nsplit = e[PKE_SPLITS], item = blockIdx.x - (int)e[PKE_ITEM0];
-    const int cols = CC * NT * cw;
+    const int cols = CC * cw;
     const int kw = (int)(blockDim.x >> 6) / cw, wk = w / cw, wc = w - wk * cw;
     const int split = nsplit == 1 ? 0 : item % nsplit;
     // the first blocks' loads wait for nothing else
@@ -284,84 +353,17 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     const int cg = ncg - 1 - (nsplit == 1 ? item : item / nsplit);
     const int row0 = e[PKE_ROW0];
 
-    // this lane's columns: their row, head and number of visible keys
-    int limit[NT], row[NT], head[NT];
-    bf16x8 qv[NT][QP][KS];
-    float qsum[NT][GS];
-    int top = 0, least = 0x7fffffff;
+    // this lane's column: its row, head and number of visible keys
+    const int column = cg * cols + wc * CC + col;
+    const bool valid = column < ncols_doc;
+    const int row = valid ? column / G : 0, head = kvh * G + (valid ? column - row * G : 0);
+    const int limit = valid ? min(pk_position(t, e, row, a.rows) + 1, (int)e[PKE_KEYS]) : 0;
+    bf16x8 qv[QP][KS];
+    float qsum[GS];
+    pk_query<T, HP, QP>(a, row0 + row, head, g4, q_vec, qv, qsum);
+    int top = limit, least = valid ? limit : 0x7fffffff;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int c = cg * cols + (wc * NT + n) * CC + col;
-        const bool valid = c < ncols_doc;
-        row[n] = valid ? c / G : 0;
-        head[n] = kvh * G + (valid ? c - row[n] * G : 0);
-        limit[n] = valid ? min(pk_position(t, e, row[n], a.rows) + 1, (int)e[PKE_KEYS]) : 0;
-        top = max(top, limit[n]);
-        if (valid) least = min(least, limit[n]);
-        const size_t q0 = (size_t)(row0 + row[n]) * a.q_stride + head[n] * a.hd;
-        row[n] = valid ? row[n] : -1;
-        const T *q = (const T *)a.q + q0;
-#pragma unroll
-        for (int g = 0; g < GS; ++g) qsum[n][g] = 0.f;
-        if constexpr (QP <= 2) {
-            u32x4 u[QP][KS];
-            if (q_vec) {  // hd is a multiple of 8
-#pragma unroll
-                for (int x = 0; x < QP; ++x)
-#pragma unroll
-                    for (int s = 0; s < KS; ++s)
-                        u[x][s] = *reinterpret_cast<const u32x4 *>((x ? (const T *)a.q_lo + q0 : q) + min(32 * s + 8 * g4, a.hd - 8));
-#pragma unroll
-                for (int x = 0; x < QP; ++x)
-#pragma unroll
-                    for (int s = 0; s < KS; ++s)
-                        if (32 * s + 8 * g4 >= a.hd) u[x][s] = u32x4{0, 0, 0, 0};
-            } else {
-#pragma unroll
-                for (int x = 0; x < QP; ++x)
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        u[x][s] = u32x4{0, 0, 0, 0};
-                        for (int j = 0; j < 8; ++j) {
-                            const int d = 32 * s + 8 * g4 + j;
-                            const uint32_t v = d < a.hd ? (uint32_t)(x ? (const T *)a.q_lo + q0 : q)[d] : 0;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (k == j >> 1) u[x][s][k] |= v << (16 * (j & 1));
-                        }
-                    }
-            }
-#pragma unroll
-            for (int x = 0; x < QP; ++x)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    qv[n][x][s] = __builtin_bit_cast(bf16x8, u[x][s]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        qsum[n][s / 2] += __uint_as_float(u[x][s][j] << 16) + __uint_as_float(u[x][s][j] & 0xffff0000u);
-                }
-        } else {
-            float v[KS][8];
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[s][j] = (float)q[min(32 * s + 8 * g4 + j, a.hd - 1)];
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (32 * s + 8 * g4 + j >= a.hd) v[s][j] = 0.f;
-                    qsum[n][s / 2] += v[s][j];
-                }
-                bf16x8 p[QP];
-                pk_pieces<QP>(v[s], p);
-#pragma unroll
-                for (int x = 0; x < QP; ++x) qv[n][x][s] = p[x];
-            }
-        }
-#pragma unroll
-        for (int g = 0; g < GS; ++g) qsum[n][g] = pk_sum4(qsum[n][g]);
-    }
+    for (int g = 0; g < GS; ++g) qsum[g] = pk_sum4(qsum[g]);
     // the wavefront's last visible key, and the keys that all its columns see
 #pragma unroll
     for (int o = 1; o < CC; o *= 2) {
@@ -374,17 +376,12 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     // steps that begin before it need no mask
     const int b_full = min(b1, least / PK_BLOCK) - (SB - 1);
 
-    f32x4 o[NT][DT];
-    float m[NT], l[NT], z[NT][GS];
+    f32x4 o[DT];
+    float m = -INFINITY, l = 0.f, z[GS];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int g = 0; g < GS; ++g) z[n][g] = 0.f;
-        m[n] = -INFINITY;
-        l[n] = 0.f;
-    }
+    for (int g = 0; g < GS; ++g) z[g] = 0.f;
     const float sc = 1.4426950408889634f / sqrtf((float)a.hd);
     uint32_t mine[CL];  // all ones for this lane's copy
 #pragma unroll
@@ -395,21 +392,19 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
         constexpr bool MASKED = decltype(masked_)::value;
         const bool more = b + kw * SB < b1;
         const int key0 = b * PK_BLOCK + 16 * copy + 4 * g4;  // this lane's keys: key0 + 16 CL h + i
-        f32x4 s[NT][H];
+        f32x4 s[H];
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            f32x4 acc[NT][GS];
+            f32x4 acc[GS];
 #pragma unroll
             for (int c = 0; c < CL; ++c) {
                 const int tile = h * CL + c;
-                f32x4 one[NT][GS];
+                f32x4 one[GS];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int g = 0; g < GS; ++g) {
-                        const float i = CENTRED ? 0.f : -OFF * qsum[n][g];
-                        one[n][g] = f32x4{i, i, i, i};
-                    }
+                for (int g = 0; g < GS; ++g) {
+                    const float i = CENTRED ? 0.f : -OFF * qsum[g];
+                    one[g] = f32x4{i, i, i, i};
+                }
 #pragma unroll
                 for (int st = 0; st < KS; ++st) {
                     const PackedBlock<HP, BITS> &k = kb[tile >> 1];
@@ -417,65 +412,56 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
                     bf16x8 ka = BITS == 4 ? pk_key4(k.word(i)) : pk_bytes(k.word(2 * i), k.word(2 * i + 1));
                     if (CENTRED) ka = pk_less(ka, RAW - OFF);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int x = 0; x < QP; ++x)
-                            one[n][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qv[n][x][st], one[n][st / 2], 0, 0, 0);
+                    for (int x = 0; x < QP; ++x)
+                        one[st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qv[x][st], one[st / 2], 0, 0, 0);
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int g = 0; g < GS; ++g)
 #pragma unroll
-                    for (int g = 0; g < GS; ++g)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[n][g][i] = c == 0 || copy == c ? one[n][g][i] : acc[n][g][i];
+                    for (int i = 0; i < 4; ++i) acc[g][i] = c == 0 || copy == c ? one[g][i] : acc[g][i];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                float v = 0.f;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float v = 0.f;
-#pragma unroll
-                    for (int g = 0; g < GS; ++g) {
-                        const uint32_t u = pk_param<GS>(kpar[h], i, g);
-                        const float sk = __uint_as_float(u << 16), mk = __uint_as_float(u & 0xffff0000u);
-                        v = fmaf(CENTRED ? mk - OFF * sk : mk, qsum[n][g], fmaf(sk, acc[n][g][i], v));
-                    }
-                    s[n][h][i] = MASKED && key0 + 16 * CL * h + i >= limit[n] ? -INFINITY : v;
+                for (int g = 0; g < GS; ++g) {
+                    const uint32_t u = pk_param<GS>(kpar[h], i, g);
+                    const float sk = __uint_as_float(u << 16), mk = __uint_as_float(u & 0xffff0000u);
+                    v = fmaf(CENTRED ? mk - OFF * sk : mk, qsum[g], fmaf(sk, acc[g][i], v));
                 }
+                s[h][i] = MASKED && key0 + 16 * CL * h + i >= limit ? -INFINITY : v;
+            }
         }
         if (more) load_keys(b + kw * SB);
         // the columns' probabilities, in place
+        float mx = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float mx = -INFINITY;
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int h = 0; h < H; ++h)
+            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[h][i]);
+        mx *= sc;
+        if (__any(mx > m + 8.f)) {
+            const float mnew = fmaxf(m, pk_max4(mx));
+            const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mnew);
+            m = mnew;
+            l *= corr;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][h][i]);
-            mx *= sc;
-            if (__any(mx > m[n] + 8.f)) {
-                const float mnew = fmaxf(m[n], pk_max4(mx));
-                const float corr = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - mnew);
-                m[n] = mnew;
-                l[n] *= corr;
+            for (int g = 0; g < GS; ++g) z[g] *= corr;
 #pragma unroll
-                for (int g = 0; g < GS; ++g) z[n][g] *= corr;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[n][d] *= corr;
-            }
-            const float mu = m[n] == -INFINITY ? 0.f : m[n];
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n][h][i], sc, -mu));
-                    s[n][h][i] = p;
-                    l[n] += p;
-                }
+            for (int d = 0; d < DT; ++d) o[d] *= corr;
         }
+        const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[h][i], sc, -mu));
+                s[h][i] = p;
+                l += p;
+            }
 #pragma unroll
         for (int g = 0; g < GS; ++g) {
-            uint32_t pw[NT][H][PP][2];  // the pieces of four probabilities times scales
+            uint32_t pw[H][PP][2];  // the pieces of four probabilities times scales
 #pragma unroll
             for (int h = 0; h < H; ++h) {
                 float sv[4], mv[4];
@@ -485,36 +471,31 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
                     sv[i] = __uint_as_float(u << 16);
                     mv[i] = fmaf(-OFF, sv[i], __uint_as_float(u & 0xffff0000u));
                 }
+                float v[4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // slots that a column does not see may hold anything, a scale of NaN too
-                        const bool hide = MASKED && key0 + 16 * CL * h + i >= limit[n];
-                        v[i] = s[n][h][i] * (hide ? 0.f : sv[i]);
-                        z[n][g] = fmaf(s[n][h][i], hide ? 0.f : mv[i], z[n][g]);
-                    }
-                    pk_pieces4<PP>(v, pw[n][h]);
+                for (int i = 0; i < 4; ++i) {
+                    // slots that a column does not see may hold anything, a scale of NaN too
+                    const bool hide = MASKED && key0 + 16 * CL * h + i >= limit;
+                    v[i] = s[h][i] * (hide ? 0.f : sv[i]);
+                    z[g] = fmaf(s[h][i], hide ? 0.f : mv[i], z[g]);
                 }
+                pk_pieces4<PP>(v, pw[h]);
             }
 #pragma unroll
             for (int x = 0; x < SB; ++x) {
                 // slots 0..3 of the operand are the block's first tile's keys, 4..7 the second's
-                bf16x8 pb[NT][PP];
+                bf16x8 pb[PP];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int q = 0; q < PP; ++q) {
+                    uint32_t u[4];
 #pragma unroll
-                    for (int q = 0; q < PP; ++q) {
-                        uint32_t u[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int tile = 2 * x + k / 2;
-                            u[k] = pw[n][tile / CL][q][k & 1];
-                            if (CL > 1) u[k] &= mine[tile % CL];
-                        }
-                        pb[n][q] = pk_operand(u[0], u[1], u[2], u[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int tile = 2 * x + k / 2;
+                        u[k] = pw[tile / CL][q][k & 1];
+                        if (CL > 1) u[k] &= mine[tile % CL];
                     }
+                    pb[q] = pk_operand(u[0], u[1], u[2], u[3]);
+                }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {  // 16-dimension tiles of the group
                     const int d = 4 * g + q;
@@ -522,10 +503,8 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
                                           : pk_bytes(vb[x].word(d * 2), vb[x].word(d * 2 + 1));
                     if (CENTRED) va = pk_less(va, RAW - OFF);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int y = 0; y < PP; ++y)
-                            o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[n][y], o[n][d], 0, 0, 0);
+                    for (int y = 0; y < PP; ++y)
+                        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[y], o[d], 0, 0, 0);
                 }
             }
         }
@@ -537,89 +516,87 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
 #pragma unroll 1
     for (; b < b1; b += kw * SB) step(b, std::true_type{});
 
+    l = pk_sum4(l);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        l[n] = pk_sum4(l[n]);
+    for (int g = 0; g < GS; ++g) {
+        const float y = pk_sum4(z[g]);
 #pragma unroll
-        for (int g = 0; g < GS; ++g) {
-            const float y = pk_sum4(z[n][g]);
+        for (int q = 0; q < 4; ++q) o[4 * g + q] += y;
+    }
+    if constexpr (CL > 1) {  // the copies of a column
+        float all = fmaxf(m, pk_ror<CC>(m));
+        if (CL == 4) all = fmaxf(all, pk_ror<8>(all));
+        const float f = pk_weight(m, all);
+        m = all;
+        auto join = [&](float v) {
+            v *= f;
+            v += pk_ror<CC>(v);
+            return CL == 4 ? v + pk_ror<8>(v) : v;
+        };
+        l = join(l);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[n][4 * g + q] += y;
-        }
-        if constexpr (CL > 1) {  // the copies of a column
-            float all = fmaxf(m[n], pk_ror<CC>(m[n]));
-            if (CL == 4) all = fmaxf(all, pk_ror<8>(all));
-            const float f = pk_weight(m[n], all);
-            m[n] = all;
-            auto join = [&](float v) {
-                v *= f;
-                v += pk_ror<CC>(v);
-                return CL == 4 ? v + pk_ror<8>(v) : v;
-            };
-            l[n] = join(l[n]);
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[n][d][i] = join(o[n][d][i]);
-        }
+            for (int i = 0; i < 4; ++i) o[d][i] = join(o[d][i]);
     }
     // Lane: one column, dimensions 16 d + 4 g4 + i.  The wavefronts of a tile hand their
     // states to each other through LDS, and wavefront wk finishes the dimension tiles wk,
     // wk + kw, ..
-    float *const mg = merge + (size_t)wc * NT * ST * 64 + lane;
-    const int mstep = cw * NT * ST * 64;
+    float *const mg = merge + (size_t)wc * ST * 64 + lane;
+    const int mstep = cw * ST * 64;
+    float *own = mg + wk * mstep;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float *p = mg + wk * mstep + n * ST * 64;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[(d * 4 + i) * 64] = o[n][d][i];
-        p[DT * 4 * 64] = m[n];
-        p[(DT * 4 + 1) * 64] = l[n];
-    }
+        for (int i = 0; i < 4; ++i) own[(d * 4 + i) * 64] = o[d][i];
+    own[DT * 4 * 64] = m;
+    own[(DT * 4 + 1) * 64] = l;
     __syncthreads();
+    if (!valid || copy > 0) return;
+    const float *p = mg;
+    float all = -INFINITY, sum = 0.f, f[PK_WAVES_MAX];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (row[n] < 0 || copy > 0) continue;
-        const float *p = mg + n * ST * 64;
-        float all = -INFINITY, sum = 0.f, f[PK_WAVES_MAX];
+    for (int k = 0; k < PK_WAVES_MAX; ++k) f[k] = k < kw ? p[k * mstep + DT * 4 * 64] : -INFINITY;
 #pragma unroll
-        for (int k = 0; k < PK_WAVES_MAX; ++k) f[k] = k < kw ? p[k * mstep + DT * 4 * 64] : -INFINITY;
+    for (int k = 0; k < PK_WAVES_MAX; ++k) all = fmaxf(all, f[k]);
 #pragma unroll
-        for (int k = 0; k < PK_WAVES_MAX; ++k) all = fmaxf(all, f[k]);
-#pragma unroll
-        for (int k = 0; k < PK_WAVES_MAX; ++k) {
-            f[k] = pk_weight(f[k], all);
-            if (k < kw) sum += p[k * mstep + (DT * 4 + 1) * 64] * f[k];
-        }
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        const int c = (wc * NT + n) * CC + col;
-        float *part = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * cols + c) * (HP + 4);
+    for (int k = 0; k < PK_WAVES_MAX; ++k) {
+        f[k] = pk_weight(f[k], all);
+        if (k < kw) sum += p[k * mstep + (DT * 4 + 1) * 64] * f[k];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    float *part = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * cols + wc * CC + col) * (HP + 4);
 #pragma unroll 1
-        for (int d = wk; d < DT; d += kw) {
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int d = wk; d < DT; d += kw) {
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < PK_WAVES_MAX; ++k)
-                if (k < kw) {
+        for (int k = 0; k < PK_WAVES_MAX; ++k)
+            if (k < kw) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] += p[k * mstep + (d * 4 + i) * 64] * f[k];
-                }
-            const int dim = 16 * d + 4 * g4;
-            if (nsplit > 1) *reinterpret_cast<f32x4 *>(part + dim) = y;
-            else if (dim < a.hd) pk_store<T>(a, row0 + row[n], head[n] * a.hd + dim, min(4, a.hd - dim), o_vec, y * inv);
-        }
-        if (nsplit > 1 && g4 == 0 && wk == 0) {
-            part[HP] = all;
-            part[HP + 1] = sum;
-        }
+                for (int i = 0; i < 4; ++i) y[i] += p[k * mstep + (d * 4 + i) * 64] * f[k];
+            }
+        const int dim = 16 * d + 4 * g4;
+        if (nsplit > 1) *reinterpret_cast<f32x4 *>(part + dim) = y;
+        else if (dim < a.hd) pk_store<T>(a, row0 + row, head * a.hd + dim, min(4, a.hd - dim), o_vec, y * inv);
+    }
+    if (nsplit > 1 && g4 == 0 && wk == 0) {
+        part[HP] = all;
+        part[HP + 1] = sum;
     }
 }
 
-template <typename T, int HP, int BITS, int QP, int NT, int CL>
+// Whether query and output rows can be moved in 16-byte (output, bf16: 8-byte) pieces.
+inline void pk_vectors(bool bf16, const PackedAttnArgs &a, bool *q_vec, bool *o_vec) {
+    const size_t es = bf16 ? 2 : 4;
+    auto aligned = [](const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; };
+    *q_vec = bf16 && a.hd % 8 == 0 && a.q_stride % 8 == 0 && aligned(a.q, 16) && aligned(a.q_lo, 16);
+    *o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && aligned(a.out, 4 * es) && aligned(a.out_lo, 4 * es);
+}
+
+template <typename T, int HP, int BITS, int QP, int CL>
 hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s) {
-    const uint32_t lds = (uint32_t)sh.waves * NT * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, NT, CL>), dim3(a.n_items, a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
+    const uint32_t lds = (uint32_t)sh.waves * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
+    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.n_items, a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
                sh.cw, (int)q_vec, (int)o_vec);
     return hipGetLastError();
 }
@@ -627,9 +604,9 @@ hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape 
 template <typename T, int HP, int BITS, int QP>
 hipError_t pk_launch_copies(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec,
                             hipStream_t s) {
-    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 1, 4>(t, a, sh, q_vec, o_vec, s);
-    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 1, 2>(t, a, sh, q_vec, o_vec, s);
-    return pk_launch<T, HP, BITS, QP, 1, 1>(t, a, sh, q_vec, o_vec, s);
+    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 4>(t, a, sh, q_vec, o_vec, s);
+    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 2>(t, a, sh, q_vec, o_vec, s);
+    return pk_launch<T, HP, BITS, QP, 1>(t, a, sh, q_vec, o_vec, s);
 }
 
 template <int HP, int BITS>
@@ -642,10 +619,8 @@ hipError_t pk_launch_bits(bool bf16, PackedShape sh, const PackedTable &t, const
 
 template <int HP>
 hipError_t pk_launch_width(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
-    const size_t es = bf16 ? 2 : 4;
-    auto aligned = [](const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; };
-    const bool q_vec = bf16 && a.hd % 8 == 0 && a.q_stride % 8 == 0 && aligned(a.q, 16) && aligned(a.q_lo, 16);
-    const bool o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && aligned(a.out, 4 * es) && aligned(a.out_lo, 4 * es);
+    bool q_vec, o_vec;
+    pk_vectors(bf16, a, &q_vec, &o_vec);
     return bits == 4 ? pk_launch_bits<HP, 4>(bf16, sh, t, a, q_vec, o_vec, s)
                      : pk_launch_bits<HP, 8>(bf16, sh, t, a, q_vec, o_vec, s);
 }

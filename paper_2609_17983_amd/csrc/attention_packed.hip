@@ -86,13 +86,17 @@ __global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedTab
 
 hipError_t launch_attention_packed64(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                      hipStream_t s);
+hipError_t launch_attention_packed_rows(int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s);
 
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                    hipStream_t s) {
     if (a.n_items <= 0) return hipSuccess;
+    if (a.hd > 128 || (bits != 4 && bits != 8) || a.n_docs < 1 || a.n_docs > PK_MAX_DOCS || a.range % PK_BLOCK != 0)
+        return hipErrorInvalidValue;
+    if (sh.tiled) return bf16 ? launch_attention_packed_rows(bits, sh, t, a, s) : hipErrorInvalidValue;
     // (a step is two blocks where a tile holds four copies)
-    if (a.hd > 128 || (bits != 4 && bits != 8) || a.n_docs > PK_MAX_DOCS || sh.nt != 1 || sh.cw < 1 || sh.waves % sh.cw != 0 ||
-        sh.waves > PK_WAVES_MAX || (sh.copies != 1 && sh.copies != 2 && sh.copies != 4) ||
+    if (sh.cw < 1 || sh.waves % sh.cw != 0 || sh.waves > PK_WAVES_MAX ||
+        (sh.copies != 1 && sh.copies != 2 && sh.copies != 4) || (sh.copies > 1 && sh.cw > 1) ||
         a.range % (PK_BLOCK * (sh.copies == 4 ? 2 : 1)) != 0)
         return hipErrorInvalidValue;
     return pk_width(a.hd) == 64 ? launch_attention_packed64(bf16, bits, sh, t, a, s)
@@ -102,15 +106,14 @@ hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const Pa
 hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                            hipStream_t s) {
     const int cols = pk_cols(sh);
-    const size_t es = bf16 ? 2 : 4;
-    const int o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && ((uintptr_t)a.out & (4 * es - 1)) == 0 &&
-                      ((uintptr_t)a.out_lo & (4 * es - 1)) == 0;
+    bool q_vec, o_vec;
+    pk_vectors(bf16, a, &q_vec, &o_vec);
     const int wc = a.max_splits > 8 ? 4 : 1;
     const dim3 grid((unsigned)(((size_t)a.n_cg * cols * wc + 3) / 4), a.Hkv);
 #define KVR_COMBINE(T, HP)                                                                                                    \
     do {                                                                                                                      \
-        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, t, a, cols, o_vec);       \
-        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, t, a, cols, o_vec);               \
+        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, t, a, cols, (int)o_vec);       \
+        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, t, a, cols, (int)o_vec);               \
     } while (0)
     if (pk_width(a.hd) == 64) {
         if (bf16) KVR_COMBINE(bf16_t, 64);

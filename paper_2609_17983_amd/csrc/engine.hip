@@ -624,9 +624,11 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
     int most = 0;
     for (int i = 0; i < n_docs; ++i) most = std::max(most, doc(i).n);
     const long long most_cols = (long long)most * G;
-    PackedShape sh{1, 1, 1, 4};
+    PackedShape sh{1, 1, 8, 0};
     if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
+    else if (c->bf16 && most_cols > env_int("KVR_PK_ROWS", 64)) sh.tiled = most_cols > 128 ? 2 : 1;
     else sh.cw = most_cols <= 32 ? 2 : 4;
+    if (sh.tiled && env_int("KVR_PK_NT", 0)) sh.tiled = env_int("KVR_PK_NT", 0);
     const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
     long long items = 0, units = 0;
     int longest = 0;
@@ -649,8 +651,8 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
     //   is a block for every unit (1237 rows: 43, split 66-80).
     const int steps = 4 * sb;
     const bool large = most_cols <= 16 && units >= 6ll * 768 * steps;
-    sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
-    const int kw = sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
+    if (!sh.tiled) sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
+    const int kw = sh.tiled ? 4 : sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
     long long range = pk_blocks(std::max(longest, 1));
     if (large || items < 256) range = std::min(range, std::max<long long>(2 * kw * sb, (units + target - 1) / target));
     range = (range + sb - 1) / sb * sb;

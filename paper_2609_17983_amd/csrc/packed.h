@@ -112,11 +112,13 @@ struct PackedAttnArgs {
     int32_t range;          // keys of a key range (a multiple of a step's)
     int32_t max_splits;     // largest number of key ranges of a document
 };
-// A block of `waves` wavefronts: cw of them hold nt column tiles each, with the
-// columns (row, query head of the kv head's group) `copies` times in a tile; the
-// waves / cw wavefronts of a tile take alternate key blocks.
-struct PackedShape { int nt, cw, copies, waves; };
-constexpr int pk_cols(PackedShape s) { return 16 / s.copies * s.nt * s.cw; }
+// A block of `waves` wavefronts: cw of them hold a column tile each, with the columns
+// (row, query head of the kv head's group) `copies` times in it; the waves / cw
+// wavefronts of a tile take alternate key blocks.  Or, `tiled` column tiles per
+// wavefront (0: the above): all wavefronts go through the keys together
+// (attention_packed_rows.hip).
+struct PackedShape { int cw, copies, waves, tiled; };
+constexpr int pk_cols(PackedShape s) { return s.tiled ? 16 * s.tiled * s.waves : 16 / s.copies * s.cw; }
 constexpr int PK_WAVES_MAX = 8;
 constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
@@ -128,13 +130,14 @@ hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const Pack
 // Entry of a launch that holds index `x`: the last one whose word `word` is not
 // above it.  Every lane looks at one entry, so the search is one load deep.
 __device__ __forceinline__ int pk_find(const PackedTable &t, int n_docs, int word, int x) {
+    if (n_docs == 1) return 0;
     const int lane = threadIdx.x & 63;
-    int n = 0;
+    constexpr int B = (PK_MAX_DOCS + 63) / 64;
+    int v[B], n = 0;
 #pragma unroll
-    for (int b = 0; b < (PK_MAX_DOCS + 63) / 64; ++b) {
-        const int i = b * 64 + lane;
-        n += __popcll(__ballot(i < n_docs && (int)t.w[i * PK_ENTRY + word] <= x));
-    }
+    for (int b = 0; b < B; ++b) v[b] = (int)t.w[min(b * 64 + lane, n_docs - 1) * PK_ENTRY + word];
+#pragma unroll
+    for (int b = 0; b < B; ++b) n += __popcll(__ballot(b * 64 + lane < n_docs && v[b] <= x));
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 __device__ __forceinline__ char *pk_pointer(const uint32_t *e) {

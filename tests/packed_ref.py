@@ -141,7 +141,7 @@ def attend(q: np.ndarray, positions, k: np.ndarray, v: np.ndarray) -> np.ndarray
     return out
 
 
-def attend_bound(q, positions, kc, vc, bits: int, fp32: bool) -> np.ndarray:
+def attend_bound(q, positions, kc, vc, bits: int, fp32: bool, pairs: bool = False) -> np.ndarray:
     """Bound on |kernel - attend| per row and head [R, Hq], without the output's own rounding; kc, vc: (codes, scale,
     offset) of the keys and values.
 
@@ -151,7 +151,10 @@ def attend_bound(q, positions, kc, vc, bits: int, fp32: bool) -> np.ndarray:
         dS <= (hd + 16) u A, plus 4 u |S| <= 4 u A from the scaling into the exponent and 2^-22 for the exponential
       probability: off by dS + 2^-22 relative; numerator and denominator both: twice that times V
       p s as bf16 pieces: 2 pieces 2^-16, 3 pieces 2^-24 of a term, relative: times V
-      the sums over n keys: at most n / 32 + 64 additions in a row, u of a partial sum each: times V, for both."""
+      the sums over n keys: at most n / 32 + 64 additions in a row, u of a partial sum each: times V, for both
+    pairs: the kernel for many rows holds keys, values and probabilities as sums of two bf16, each off by 2^-16 relative
+      (half a step of the second piece, 2^-8 of at most 2^-8), and leaves out the product of the two second pieces of
+      values and probabilities, 2^-16: dS <= 2^-16 A more, outputs 2 * 2^-16 V more."""
     u = 2.0 ** -24
     big = 32.0 if bits == 4 else 256.0
     R, Hq, hd = q.shape
@@ -167,6 +170,7 @@ def attend_bound(q, positions, kc, vc, bits: int, fp32: bool) -> np.ndarray:
             K = float((big * kc[1][g, :n].astype(F64) + np.abs(kc[2][g, :n].astype(F64))).max())
             V = float((big * vc[1][g, :n].astype(F64) + np.abs(vc[2][g, :n].astype(F64))).max())
             A = float(np.abs(q[r, h].astype(F64)).sum()) * K / np.sqrt(hd)
-            dS = (hd + 20) * u * A + 2.0 ** -22
-            out[r, h] = V * (2 * (dS + 2.0 ** -22) + (u if fp32 else 2.0 ** -16) + 2 * (n / 32 + 64) * u)
+            dS = ((hd + 20) * u + (2.0 ** -16 if pairs else 0.0)) * A + 2.0 ** -22
+            out[r, h] = V * (2 * (dS + 2.0 ** -22) + (u if fp32 else 2.0 ** -16) +
+                             (2.0 ** -15 if pairs else 0.0) + 2 * (n / 32 + 64) * u)
     return out
