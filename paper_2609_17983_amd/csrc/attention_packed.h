@@ -318,9 +318,9 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / CC, col = (lane & 15) % CC;
-    const int kvh = blockIdx.y;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.x) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = blockIdx.x - (int)e[PKE_ITEM0];
+    const int kvh = blockIdx.x;
+    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.y) * PK_ENTRY;
+    const int nsplit = e[PKE_SPLITS], item = blockIdx.y - (int)e[PKE_ITEM0];
     const int cols = CC * cw;
     const int kw = (int)(blockDim.x >> 6) / cw, wk = w / cw, wc = w - wk * cw;
     const int split = nsplit == 1 ? 0 : item % nsplit;
@@ -596,7 +596,7 @@ inline void pk_vectors(bool bf16, const PackedAttnArgs &a, bool *q_vec, bool *o_
 template <typename T, int HP, int BITS, int QP, int CL>
 hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s) {
     const uint32_t lds = (uint32_t)sh.waves * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.n_items, a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
+    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, t, a,
                sh.cw, (int)q_vec, (int)o_vec);
     return hipGetLastError();
 }

@@ -21,8 +21,6 @@ namespace kvr {
 
 namespace {
 
-constexpr int PR_WAVES = 8;
-
 // Eight values as a pair of operands.
 __device__ __forceinline__ void pr_split(const float v[8], u32x4 *hi, u32x4 *lo) {
     bf16x8 p[2];
@@ -31,12 +29,11 @@ __device__ __forceinline__ void pr_split(const float v[8], u32x4 *hi, u32x4 *lo)
     *lo = __builtin_bit_cast(u32x4, p[1]);
 }
 
-// NT: column tiles of a wavefront.
-template <int HP, int BITS, int QP, int NT>
+template <int HP, int BITS, int QP>
 __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(PackedTable t, PackedAttnArgs a, int q_vec,
                                                                              int o_vec) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
-    constexpr int COLS = 16 * NT * PR_WAVES;
+    constexpr int NT = PR_TILES, COLS = pk_cols(PACKED_ROWS);
     // operands of a key block: keys [16-key tile][step][lane], values [16-dimension tile][lane]
     constexpr int KU = 2 * KS, VU = DT;
     static_assert(KU == VU && KU + VU == (HP == 128 ? 2 : 1) * PR_WAVES, "operands of a block over the wavefronts");
@@ -45,9 +42,9 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     int *const flags = reinterpret_cast<int *>(lds + 2 * BUF);
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kvh = blockIdx.y;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.x) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = blockIdx.x - (int)e[PKE_ITEM0];
+    const int kvh = blockIdx.x;
+    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.y) * PK_ENTRY;
+    const int nsplit = e[PKE_SPLITS], item = blockIdx.y - (int)e[PKE_ITEM0];
     const int split = nsplit == 1 ? 0 : item % nsplit;
     const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
     const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
@@ -61,7 +58,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     const int ku = w, vu = HP == 128 ? w : w - KU;  // operand index
     uint32_t kword[BITS / 4], vword[2];
     uint32_t kpar;
-    u32x4 vpar[2][GS];
+    u32x4 vpar[2][GS];  // GS words a position: elements 0 and 2 (one group: all) are the operand's group
     auto fetch = [&](int b) {
         const char *kblk = kp + (size_t)min(b, last) * BB, *vblk = vp + (size_t)min(b, last) * BB;
         if (has_key) {
@@ -76,8 +73,19 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
             const uint32_t *p = reinterpret_cast<const uint32_t *>(vblk) + (lane * (BITS == 4 ? KS : DT) + (BITS == 4 ? vu >> 1 : vu)) * 2;
             vword[0] = p[0];
             vword[1] = p[1];
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(vblk + CB) + (GS > 1 ? vu / 4 : 0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) pk_params<HP, BITS>(vpar[h], vp, min(b, last), h, g4);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < GS; ++i) {
+                    const uint32_t *r = q + (16 * h + 4 * g4) * GS + 4 * i;
+                    if constexpr (GS == 1) {
+                        vpar[h][i] = *reinterpret_cast<const u32x4 *>(r);
+                    } else {
+                        vpar[h][i][0] = r[0];
+                        vpar[h][i][2] = r[2];
+                    }
+                }
         }
     };
     // The fetched block's operands into a buffer.
@@ -88,31 +96,39 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
             const float s = __uint_as_float(kpar << 16), m = __uint_as_float(kpar & 0xffff0000u);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t c = BITS == 4 ? kword[0] >> (4 * ((j & 1) * 4 + (j >> 1))) & 15u : kword[j >> 2] >> (8 * (j & 3)) & 0xffu;
-                v[j] = fmaf(s, (float)c, m);
+                // 4 bits: nibble (j%2) * 4 + j/2, in byte 2 (j%2) + j/4
+                const uint32_t word = BITS == 4 ? kword[0] >> (4 * (j >> 1 & 1)) & 0x0f0f0f0fu : kword[BITS == 4 ? 0 : j >> 2];
+                const int byte = BITS == 4 ? 2 * (j & 1) + (j >> 2) : j & 3;
+                v[j] = fmaf(s, (float)(word >> (8 * byte) & 0xffu), m);
             }
             pr_split(v, base + ku * 64 + lane, base + (KU + VU + ku) * 64 + lane);
         }
         if (has_value) {
             float v[8];
-            const int g = vu / 4;  // group of the dimensions
-            uint32_t slots = 0;    // this lane's slots whose value is not finite (or is infinite as bf16)
+            uint32_t t = 0;  // an offset of 2^125 or a scale of 2^119 or more (or NaN) carries into the sign bits
+            const uint32_t c4[2] = {BITS == 4 ? vword[0] >> (4 * (vu & 1)) & 0x0f0f0f0fu : vword[0],
+                                    BITS == 4 ? vword[1] >> (4 * (vu & 1)) & 0x0f0f0f0fu : vword[1]};
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int h = j >> 2, i = j & 3, r = 16 * h + 4 * g4 + i;
-                const uint32_t u = pk_param<GS>(vpar[h], i, 0), u1 = GS > 1 ? pk_param<GS>(vpar[h], i, GS - 1) : u;
-                const uint32_t par = g ? u1 : u;
-                const uint32_t c = BITS == 4 ? vword[h] >> (8 * i + 4 * (vu & 1)) & 15u : vword[h] >> (8 * i) & 0xffu;
-                v[j] = fmaf(__uint_as_float(par << 16), (float)c, __uint_as_float(par & 0xffff0000u));
-                if (!(fabsf(v[j]) < 3.38e38f)) {
-                    v[j] = 0.f;
-                    slots |= 1u << r;
-                }
+                const int h = j >> 2, i = j & 3;
+                const uint32_t u = GS == 1 ? vpar[h][0][i] : vpar[h][i >> 1][2 * (i & 1)];
+                v[j] = fmaf(__uint_as_float(u << 16), (float)(c4[h] >> (8 * i) & 0xffu), __uint_as_float(u & 0xffff0000u));
+                t |= (u & 0x7f807f80u) + 0x02000500u;
             }
-            // slots behind the last position that any row sees hold anything
-            const int seen = min(keys - b * PK_BLOCK, PK_BLOCK);
-            slots &= 0xffffffffu >> (32 - seen);
-            if (slots) atomicOr(&flags[buf * 2 + g], (int)slots);
+            if (__any((t & 0x80008000u) != 0)) {
+                // values that are not finite (or are infinite as bf16), in this lane's slots
+                uint32_t slots = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (!(fabsf(v[j]) < 3.38e38f)) {
+                        v[j] = 0.f;
+                        slots |= 1u << (16 * (j >> 2) + 4 * g4 + (j & 3));
+                    }
+                // slots behind the last position that any row sees hold anything
+                const int seen = min(keys - b * PK_BLOCK, PK_BLOCK);
+                slots &= 0xffffffffu >> (32 - seen);
+                if (slots) atomicOr(&flags[buf * 2 + (GS > 1 ? vu / 4 : 0)], (int)slots);
+            }
             pr_split(v, base + (KU + vu) * 64 + lane, base + (KU + VU + KU + vu) * 64 + lane);
         }
     };
@@ -175,11 +191,19 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     for (int b = b0; b < b1; ++b) {
         const int buf = (b - b0) & 1;
         __syncthreads();  // block b is staged; nobody reads the other buffer any more
-        if (b + 1 < b1) {
-            stage(b + 1, buf ^ 1);
-            if (b + 2 < b1) fetch(b + 2);
+        // half of the wavefronts (one of two on a SIMD) stage the next block before their
+        // products, half after them: vector and matrix instructions then run side by side
+        auto next = [&] {
+            if (b + 1 < b1) {
+                stage(b + 1, buf ^ 1);
+                if (b + 2 < b1) fetch(b + 2);
+            }
+        };
+        if (w < PR_WAVES / 2) next();
+        if (b * PK_BLOCK >= top) {  // none of this wavefront's columns sees it
+            if (w >= PR_WAVES / 2) next();
+            continue;
         }
-        if (b * PK_BLOCK >= top) continue;  // none of this wavefront's columns sees it
         const u32x4 *const base = lds + buf * BUF;
         f32x4 s[NT][2];
 #pragma unroll
@@ -263,6 +287,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
                 }
             }
         }
+        if (w >= PR_WAVES / 2) next();
     }
     // lane: column lane%16, dimensions 16 d + 4 g4 + i
 #pragma unroll
@@ -286,25 +311,21 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
 }
 
 template <int HP, int BITS>
-hipError_t pr_launch(int nt, const PackedTable &t, const PackedAttnArgs &a, bool q_vec, bool o_vec, hipStream_t s) {
-    const dim3 grid(a.n_items, a.Hkv), block(64 * PR_WAVES);
+hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
+    bool q_vec, o_vec;
+    pk_vectors(true, a, &q_vec, &o_vec);
+    const dim3 grid(a.Hkv, a.n_items), block(64 * PR_WAVES);
     const uint32_t bytes = 2 * 2 * (HP / 8) * 64 * 16 + (4 + PR_WAVES) * 4;
-    if (a.q_lo && nt == 1) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2, 1>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
-    else if (a.q_lo) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2, 2>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
-    else if (nt == 1) kvr_launch((attention_packed_rows_kernel<HP, BITS, 1, 1>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
-    else kvr_launch((attention_packed_rows_kernel<HP, BITS, 1, 2>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
+    if (a.q_lo) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
+    else kvr_launch((attention_packed_rows_kernel<HP, BITS, 1>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attention_packed_rows(int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
-    if (sh.waves != PR_WAVES || (sh.tiled != 1 && sh.tiled != 2)) return hipErrorInvalidValue;
-    bool q_vec, o_vec;
-    pk_vectors(true, a, &q_vec, &o_vec);
-    if (pk_width(a.hd) == 64)
-        return bits == 4 ? pr_launch<64, 4>(sh.tiled, t, a, q_vec, o_vec, s) : pr_launch<64, 8>(sh.tiled, t, a, q_vec, o_vec, s);
-    return bits == 4 ? pr_launch<128, 4>(sh.tiled, t, a, q_vec, o_vec, s) : pr_launch<128, 8>(sh.tiled, t, a, q_vec, o_vec, s);
+hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
+    if (pk_width(a.hd) == 64) return bits == 4 ? pr_launch<64, 4>(t, a, s) : pr_launch<64, 8>(t, a, s);
+    return bits == 4 ? pr_launch<128, 4>(t, a, s) : pr_launch<128, 8>(t, a, s);
 }
 
 }  // namespace kvr

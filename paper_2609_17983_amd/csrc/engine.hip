@@ -621,44 +621,53 @@ template <typename DocAt>
 void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_table) {
     const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
     t.packed.clear();
-    int most = 0;
-    for (int i = 0; i < n_docs; ++i) most = std::max(most, doc(i).n);
-    const long long most_cols = (long long)most * G;
-    PackedShape sh{1, 1, 8, 0};
-    if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
-    else if (c->bf16 && most_cols > env_int("KVR_PK_ROWS", 64)) sh.tiled = most_cols > 128 ? 2 : 1;
-    else sh.cw = most_cols <= 32 ? 2 : 4;
-    if (sh.tiled && env_int("KVR_PK_NT", 0)) sh.tiled = env_int("KVR_PK_NT", 0);
-    const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
-    long long items = 0, units = 0;
+    // the documents' rows and keys
+    struct Size { long long cols; int blocks; };
+    std::vector<Size> size(n_docs);
+    long long most_cols = 0, wide = 0;
     int longest = 0;
     for (int i = 0; i < n_docs; ++i) {
         const PackedQuery q = doc(i);
         int keys = 0;
         for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
-        const long long ncg = ((long long)q.n * G + cols - 1) / cols;
-        items += ncg * Hkv;
-        units += ncg * Hkv * pk_blocks(keys);
+        size[i] = {(long long)q.n * G, pk_blocks(keys)};
+        most_cols = std::max(most_cols, size[i].cols);
+        wide += (size[i].cols + pk_cols(PACKED_ROWS) - 1) / pk_cols(PACKED_ROWS) * Hkv;
         longest = std::max(longest, keys);
     }
-    // Key ranges (measured in us a call; 256 units hold two wavefronts per SIMD):
+    // The kernel for many rows once it has a block for every unit (us a call, it and the
+    // other: 4000-token prompt, 32 heads, 297 and 417; two of 1500 tokens 110 and 162; one
+    // of them 106 and 76).
+    PackedShape sh{1, 1, 8, false};
+    if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
+    else if (c->bf16 && wide >= env_int("KVR_PK_WIDE", 256)) sh = PACKED_ROWS;
+    else sh.cw = most_cols <= 32 ? 2 : 4;
+    const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
+    auto count = [&](long long range) {  // blocks with key ranges of `range` blocks of keys, and their number unsplit
+        long long n = 0;
+        for (const Size &z : size) n += (z.cols + cols - 1) / cols * Hkv * std::max<long long>(1, (z.blocks + range - 1) / range);
+        return n;
+    };
+    long long units = 0;
+    for (const Size &z : size) units += (z.cols + cols - 1) / cols * Hkv * z.blocks;
+    // Key ranges (us a call; a unit holds one block of eight wavefronts, two of four):
     // - much work for few columns, bound by memory: blocks of four wavefronts, about three
     //   to a unit, so that units that finish early take more (64 documents of 2000-8000
     //   positions: 85; one block per document 88, blocks of eight 90-94);
-    // - little work: blocks of eight wavefronts, one to a unit, two steps a wavefront at
-    //   least (one document of 40001 positions 18, 768 blocks 24; 48 rows 17 and 24);
-    // - many columns, whose partials cost more than an uneven end: not split once there
-    //   is a block for every unit (1237 rows: 43, split 66-80).
-    const int steps = 4 * sb;
-    const bool large = most_cols <= 16 && units >= 6ll * 768 * steps;
-    if (!sh.tiled) sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
-    const int kw = sh.tiled ? 4 : sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
-    long long range = pk_blocks(std::max(longest, 1));
-    if (large || items < 256) range = std::min(range, std::max<long long>(2 * kw * sb, (units + target - 1) / target));
-    range = (range + sb - 1) / sb * sb;
+    // - otherwise blocks of eight wavefronts, as many as there are units and no more (8
+    //   documents, 48 rows of 32 heads: 57; a second round of blocks 94), with two steps
+    //   a wavefront at least (one document of 40001 positions 18; twice the blocks 24).
+    const bool large = most_cols <= 16 && units >= 6ll * 768 * 4 * sb;
+    if (!sh.rows) sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
+    const int kw = sh.rows ? 4 : sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
+    const long long whole = (pk_blocks(std::max(longest, 1)) + sb - 1) / sb * sb;
+    long long range = std::max<long long>(2 * kw * sb, (units + target - 1) / target);
+    range = std::min(whole, (range + sb - 1) / sb * sb);
+    if (!large)
+        while (range < whole && count(range) > target) range = std::min(whole, range + std::max<long long>(range / 16 / sb * sb, sb));
     const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
-    while (range < pk_blocks(longest) && (pk_blocks(longest) + range - 1) / range * per_row > slots) range *= 2;
+    while (range < whole && (whole + range - 1) / range * per_row > slots) range = std::min(whole, range * 2);
     t.packed_shape = sh;
     t.packed_range = (int)range * PK_BLOCK;
 

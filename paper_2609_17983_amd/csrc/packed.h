@@ -114,11 +114,13 @@ struct PackedAttnArgs {
 };
 // A block of `waves` wavefronts: cw of them hold a column tile each, with the columns
 // (row, query head of the kv head's group) `copies` times in it; the waves / cw
-// wavefronts of a tile take alternate key blocks.  Or, `tiled` column tiles per
-// wavefront (0: the above): all wavefronts go through the keys together
-// (attention_packed_rows.hip).
-struct PackedShape { int cw, copies, waves, tiled; };
-constexpr int pk_cols(PackedShape s) { return s.tiled ? 16 * s.tiled * s.waves : 16 / s.copies * s.cw; }
+// wavefronts of a tile take alternate key blocks.  rows: the kernel for many rows
+// (attention_packed_rows.hip), whose wavefronts hold PR_TILES column tiles each and go
+// through the keys together.
+struct PackedShape { int cw, copies, waves; bool rows; };
+constexpr int PR_WAVES = 8, PR_TILES = 2;
+constexpr PackedShape PACKED_ROWS = {PR_WAVES, 1, PR_WAVES, true};
+constexpr int pk_cols(PackedShape s) { return 16 / s.copies * s.cw * (s.rows ? PR_TILES : 1); }
 constexpr int PK_WAVES_MAX = 8;
 constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
