@@ -594,8 +594,11 @@ inline void pk_vectors(bool bf16, const PackedAttnArgs &a, bool *q_vec, bool *o_
 }
 
 template <typename T, int HP, int BITS, int QP, int CL>
-hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s) {
+hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s,
+                     int *resident) {
     const uint32_t lds = (uint32_t)sh.waves * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
+    static std::atomic<int> known[2];
+    if (resident) return pk_resident(attention_packed_kernel<T, HP, BITS, QP, CL>, sh.waves, lds, known, resident);
     kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, t, a,
                sh.cw, (int)q_vec, (int)o_vec);
     return hipGetLastError();
@@ -603,26 +606,27 @@ hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape 
 
 template <typename T, int HP, int BITS, int QP>
 hipError_t pk_launch_copies(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec,
-                            hipStream_t s) {
-    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 4>(t, a, sh, q_vec, o_vec, s);
-    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 2>(t, a, sh, q_vec, o_vec, s);
-    return pk_launch<T, HP, BITS, QP, 1>(t, a, sh, q_vec, o_vec, s);
+                            hipStream_t s, int *resident) {
+    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 4>(t, a, sh, q_vec, o_vec, s, resident);
+    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 2>(t, a, sh, q_vec, o_vec, s, resident);
+    return pk_launch<T, HP, BITS, QP, 1>(t, a, sh, q_vec, o_vec, s, resident);
 }
 
 template <int HP, int BITS>
 hipError_t pk_launch_bits(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, bool q_vec, bool o_vec,
-                          hipStream_t s) {
-    if (!bf16) return pk_launch_copies<float, HP, BITS, 3>(t, a, sh, q_vec, o_vec, s);
-    return a.q_lo ? pk_launch_copies<bf16_t, HP, BITS, 2>(t, a, sh, q_vec, o_vec, s)
-                  : pk_launch_copies<bf16_t, HP, BITS, 1>(t, a, sh, q_vec, o_vec, s);
+                          hipStream_t s, int *resident) {
+    if (!bf16) return pk_launch_copies<float, HP, BITS, 3>(t, a, sh, q_vec, o_vec, s, resident);
+    return a.q_lo ? pk_launch_copies<bf16_t, HP, BITS, 2>(t, a, sh, q_vec, o_vec, s, resident)
+                  : pk_launch_copies<bf16_t, HP, BITS, 1>(t, a, sh, q_vec, o_vec, s, resident);
 }
 
 template <int HP>
-hipError_t pk_launch_width(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
+hipError_t pk_launch_width(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s,
+                           int *resident) {
     bool q_vec, o_vec;
     pk_vectors(bf16, a, &q_vec, &o_vec);
-    return bits == 4 ? pk_launch_bits<HP, 4>(bf16, sh, t, a, q_vec, o_vec, s)
-                     : pk_launch_bits<HP, 8>(bf16, sh, t, a, q_vec, o_vec, s);
+    return bits == 4 ? pk_launch_bits<HP, 4>(bf16, sh, t, a, q_vec, o_vec, s, resident)
+                     : pk_launch_bits<HP, 8>(bf16, sh, t, a, q_vec, o_vec, s, resident);
 }
 
 }  // namespace

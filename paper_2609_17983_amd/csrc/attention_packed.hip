@@ -85,22 +85,22 @@ __global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedTab
 }  // namespace
 
 hipError_t launch_attention_packed64(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
-                                     hipStream_t s);
-hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s);
+                                     hipStream_t s, int *resident);
+hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident);
 
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
-                                   hipStream_t s) {
-    if (a.n_items <= 0) return hipSuccess;
-    if (a.hd > 128 || (bits != 4 && bits != 8) || a.n_docs < 1 || a.n_docs > PK_MAX_DOCS || a.range % PK_BLOCK != 0)
+                                   hipStream_t s, int *resident) {
+    if (!resident && a.n_items <= 0) return hipSuccess;
+    if (a.hd > 128 || (bits != 4 && bits != 8) || (!resident && a.n_docs < 1) || a.n_docs > PK_MAX_DOCS || a.range % PK_BLOCK != 0)
         return hipErrorInvalidValue;
-    if (sh.rows) return bf16 ? launch_attention_packed_rows(bits, t, a, s) : hipErrorInvalidValue;
+    if (sh.rows) return bf16 ? launch_attention_packed_rows(bits, t, a, s, resident) : hipErrorInvalidValue;
     // (a step is two blocks where a tile holds four copies)
-    if (sh.cw < 1 || sh.waves % sh.cw != 0 || sh.waves > PK_WAVES_MAX ||
+    if (sh.cw < 1 || sh.waves % sh.cw != 0 || (sh.waves != 4 && sh.waves != 8) ||
         (sh.copies != 1 && sh.copies != 2 && sh.copies != 4) || (sh.copies > 1 && sh.cw > 1) ||
         a.range % (PK_BLOCK * (sh.copies == 4 ? 2 : 1)) != 0)
         return hipErrorInvalidValue;
-    return pk_width(a.hd) == 64 ? launch_attention_packed64(bf16, bits, sh, t, a, s)
-                                : pk_launch_width<128>(bf16, bits, sh, t, a, s);
+    return pk_width(a.hd) == 64 ? launch_attention_packed64(bf16, bits, sh, t, a, s, resident)
+                                : pk_launch_width<128>(bf16, bits, sh, t, a, s, resident);
 }
 
 hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,

@@ -4,8 +4,8 @@
 namespace kvr {
 
 hipError_t launch_attention_packed64(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
-                                     hipStream_t s) {
-    return pk_launch_width<64>(bf16, bits, sh, t, a, s);
+                                     hipStream_t s, int *resident) {
+    return pk_launch_width<64>(bf16, bits, sh, t, a, s, resident);
 }
 
 }  // namespace kvr

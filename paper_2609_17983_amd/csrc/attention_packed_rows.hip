@@ -311,11 +311,15 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
 }
 
 template <int HP, int BITS>
-hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
+hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident) {
     bool q_vec, o_vec;
     pk_vectors(true, a, &q_vec, &o_vec);
     const dim3 grid(a.Hkv, a.n_items), block(64 * PR_WAVES);
     const uint32_t bytes = 2 * 2 * (HP / 8) * 64 * 16 + (4 + PR_WAVES) * 4;
+    static std::atomic<int> known[2][2];
+    if (resident)
+        return a.q_lo ? pk_resident(attention_packed_rows_kernel<HP, BITS, 2>, PR_WAVES, bytes, known[1], resident)
+                      : pk_resident(attention_packed_rows_kernel<HP, BITS, 1>, PR_WAVES, bytes, known[0], resident);
     if (a.q_lo) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
     else kvr_launch((attention_packed_rows_kernel<HP, BITS, 1>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
     return hipGetLastError();
@@ -323,9 +327,9 @@ hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t 
 
 }  // namespace
 
-hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s) {
-    if (pk_width(a.hd) == 64) return bits == 4 ? pr_launch<64, 4>(t, a, s) : pr_launch<64, 8>(t, a, s);
-    return bits == 4 ? pr_launch<128, 4>(t, a, s) : pr_launch<128, 8>(t, a, s);
+hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident) {
+    if (pk_width(a.hd) == 64) return bits == 4 ? pr_launch<64, 4>(t, a, s, resident) : pr_launch<64, 8>(t, a, s, resident);
+    return bits == 4 ? pr_launch<128, 4>(t, a, s, resident) : pr_launch<128, 8>(t, a, s, resident);
 }
 
 }  // namespace kvr

@@ -616,9 +616,10 @@ struct PackedQuery {
 };
 
 // The attention launches of rows over packed caches (t.packed): which columns a
-// block takes, and into how many key ranges a document's keys are cut.
+// block takes, and into how many key ranges a document's keys are cut.  pair: the
+// queries are compensated pairs.
 template <typename DocAt>
-void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_table) {
+hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_docs, DocAt doc, bool row_table) {
     const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
     t.packed.clear();
     // the documents' rows and keys
@@ -640,7 +641,7 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
     // of them 106 and 76).
     PackedShape sh{1, 1, 8, false};
     if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
-    else if (c->bf16 && wide >= env_int("KVR_PK_WIDE", 256)) sh = PACKED_ROWS;
+    else if (c->bf16 && wide >= 256) sh = PACKED_ROWS;
     else sh.cw = most_cols <= 32 ? 2 : 4;
     const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
     auto count = [&](long long range) {  // blocks with key ranges of `range` blocks of keys, and their number unsplit
@@ -650,21 +651,26 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
     };
     long long units = 0;
     for (const Size &z : size) units += (z.cols + cols - 1) / cols * Hkv * z.blocks;
-    // Key ranges (us a call; a unit holds one block of eight wavefronts, two of four):
-    // - much work for few columns, bound by memory: blocks of four wavefronts, about three
-    //   to a unit, so that units that finish early take more (64 documents of 2000-8000
-    //   positions: 85; one block per document 88, blocks of eight 90-94);
-    // - otherwise blocks of eight wavefronts, as many as there are units and no more (8
-    //   documents, 48 rows of 32 heads: 57; a second round of blocks 94), with two steps
-    //   a wavefront at least (one document of 40001 positions 18; twice the blocks 24).
+    // Key ranges: as many blocks as the device holds at a time and no more, so that none
+    // waits for a second round (us a call, with as many blocks and with half as many
+    // again: 64 documents of 2000-8000 positions, 32 heads, 80 and 98; 60 documents, 28
+    // heads, 48 and 55; 8 documents of 48 rows 57 and 94), and two steps a wavefront at
+    // least.  Little work takes blocks of eight wavefronts, whose partials are fewer (one
+    // document of 40001 positions 17.5, blocks of four 18.7); much work for few columns
+    // blocks of four, which come out more even (64 documents 80 and 90).
     const bool large = most_cols <= 16 && units >= 6ll * 768 * 4 * sb;
-    if (!sh.rows) sh.waves = env_int("KVR_PK_WAVES", large ? 4 : 8);
-    const int kw = sh.rows ? 4 : sh.waves / sh.cw, target = env_int("KVR_PK_TARGET", large ? 768 : 256);
+    if (large) sh.waves = 4;
+    const int kw = sh.rows ? 4 : sh.waves / sh.cw;
+    PackedAttnArgs probe{};
+    probe.hd = c->d.head_dim;
+    probe.q_lo = pair ? c->Qb_lo : nullptr;
+    int target = 0;
+    const hipError_t err = launch_attention_packed(c->bf16, bits, sh, PackedTable{}, probe, nullptr, &target);
+    if (err != hipSuccess) return err;
     const long long whole = (pk_blocks(std::max(longest, 1)) + sb - 1) / sb * sb;
     long long range = std::max<long long>(2 * kw * sb, (units + target - 1) / target);
     range = std::min(whole, (range + sb - 1) / sb * sb);
-    if (!large)
-        while (range < whole && count(range) > target) range = std::min(whole, range + std::max<long long>(range / 16 / sb * sb, sb));
+    while (range < whole && count(range) > target) range = std::min(whole, range + std::max<long long>(range / 16 / sb * sb, sb));
     const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
     while (range < whole && (whole + range - 1) / range * per_row > slots) range = std::min(whole, range * 2);
@@ -715,6 +721,7 @@ void plan_packed(const kvr_ctx *c, Tables &t, int n_docs, DocAt doc, bool row_ta
             q.n -= n;
         }
     }
+    return hipSuccess;
 }
 
 // The kernel arguments of one of plan_packed's launches; `a` describes the rows.
@@ -744,13 +751,15 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
     const bool attn_mfma = !c->force_simple && attention_mfma_ok(c->bf16, d.n_heads, d.n_kv_heads, d.head_dim);
     const bool sk = skinny_pass_ok(c, R);
     const bool op = c->wpk != nullptr;  // matrix operands in MFMA operand order (both packed-weight kernels)
-    if (bits)
-        plan_packed(c, t, (int)t.docs.size(), [&](int i) {
+    if (bits) {
+        const hipError_t err = plan_packed(c, t, bits, c->bf16, (int)t.docs.size(), [&](int i) {
             const DocInfo &dc = t.docs[i];
             return PackedQuery{dc.cache, dc.n_cap, dc.row0, dc.nrows, &t.rows[dc.row0].pos, (int)(sizeof(RowInfo) / 4)};
         }, true);
-    else
+        if (err != hipSuccess) return hip_fail(c, err, "attention plan");
+    } else {
         plan_attention(c, t, attn_mfma);
+    }
     if ((int)t.items.size() > c->items_cap || (int)t.comb.size() > c->comb_cap)
         return fail(c, KVR_E_RANGE, "attention plan exceeds the context's item capacity");
 
@@ -1885,9 +1894,10 @@ static kvr_status attention_packed(kvr_ctx *c, int32_t layer, int32_t bits, cons
     t.clear();
     std::vector<int> row0(n_docs);
     for (int i = 0, r = 0; i < n_docs; r += docs[i++].n_rows) row0[i] = r;
-    plan_packed(c, t, n_docs, [&](int i) {
+    const hipError_t err = plan_packed(c, t, bits, false, n_docs, [&](int i) {
         return PackedQuery{docs[i].d_packed, docs[i].n_cap, row0[i], docs[i].n_rows, docs[i].h_positions, 1};
     }, false);
+    if (err != hipSuccess) return hip_fail(c, err, "kvr_attention_packed");
     PackedAttnArgs a{};
     a.q = d_q; a.q_stride = q_stride;
     a.out = d_out; a.out_stride = out_stride;

@@ -3,6 +3,8 @@
 // over them.
 #pragma once
 
+#include <atomic>
+
 #include "common.h"
 
 namespace kvr {
@@ -123,8 +125,27 @@ constexpr PackedShape PACKED_ROWS = {PR_WAVES, 1, PR_WAVES, true};
 constexpr int pk_cols(PackedShape s) { return 16 / s.copies * s.cw * (s.rows ? PR_TILES : 1); }
 constexpr int PK_WAVES_MAX = 8;
 constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
+// resident given: nothing is launched, and it receives the number of blocks that a
+// device holds at a time (only hd and q_lo of `a` are looked at).
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
-                                   hipStream_t s);
+                                   hipStream_t s, int *resident = nullptr);
+// Launch a block of `waves` wavefronts with `lds` bytes, or answer *resident.  `known`:
+// the answers so far, by waves / 4 - 1.
+template <typename K>
+inline hipError_t pk_resident(K kernel, int waves, size_t lds, std::atomic<int> *known, int *resident) {
+    int n = known[waves / 4 - 1].load(std::memory_order_relaxed);
+    if (n == 0) {
+        int dev = 0, units = 0, blocks = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e == hipSuccess) e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, 64 * waves, lds);
+        if (e != hipSuccess) return e;
+        n = units * (blocks > 0 ? blocks : 1);
+        known[waves / 4 - 1].store(n, std::memory_order_relaxed);
+    }
+    *resident = n;
+    return hipSuccess;
+}
 hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                            hipStream_t s);
 
