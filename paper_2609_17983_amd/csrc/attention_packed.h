@@ -318,9 +318,10 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / CC, col = (lane & 15) % CC;
-    const int kvh = blockIdx.x;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.y) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = blockIdx.y - (int)e[PKE_ITEM0];
+    // kv heads first: the longest items of all of them start before the shorter ones
+    const int kvh = blockIdx.x % a.Hkv, index = blockIdx.x / a.Hkv;
+    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, index) * PK_ENTRY;
+    const int nsplit = e[PKE_SPLITS], item = index - (int)e[PKE_ITEM0];
     const int cols = CC * cw;
     const int kw = (int)(blockDim.x >> 6) / cw, wk = w / cw, wc = w - wk * cw;
     const int split = nsplit == 1 ? 0 : item % nsplit;
@@ -599,7 +600,7 @@ hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape 
     const uint32_t lds = (uint32_t)sh.waves * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
     static std::atomic<int> known[2];
     if (resident) return pk_resident(attention_packed_kernel<T, HP, BITS, QP, CL>, sh.waves, lds, known, resident);
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, t, a,
+    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.n_items * a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
                sh.cw, (int)q_vec, (int)o_vec);
     return hipGetLastError();
 }

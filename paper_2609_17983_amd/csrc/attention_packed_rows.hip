@@ -42,9 +42,10 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     int *const flags = reinterpret_cast<int *>(lds + 2 * BUF);
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kvh = blockIdx.x;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, blockIdx.y) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = blockIdx.y - (int)e[PKE_ITEM0];
+    // kv heads first: the longest items of all of them start before the shorter ones
+    const int kvh = blockIdx.x % a.Hkv, index = blockIdx.x / a.Hkv;
+    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, index) * PK_ENTRY;
+    const int nsplit = e[PKE_SPLITS], item = index - (int)e[PKE_ITEM0];
     const int split = nsplit == 1 ? 0 : item % nsplit;
     const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
     const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
@@ -314,7 +315,7 @@ template <int HP, int BITS>
 hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident) {
     bool q_vec, o_vec;
     pk_vectors(true, a, &q_vec, &o_vec);
-    const dim3 grid(a.Hkv, a.n_items), block(64 * PR_WAVES);
+    const dim3 grid(a.n_items * a.Hkv), block(64 * PR_WAVES);
     const uint32_t bytes = 2 * 2 * (HP / 8) * 64 * 16 + (4 + PR_WAVES) * 4;
     static std::atomic<int> known[2][2];
     if (resident)

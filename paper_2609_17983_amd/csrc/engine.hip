@@ -563,10 +563,10 @@ struct TableFill {
         e[PKE_POS] = (uint32_t)pos[0];
         return k;
     }
-    // An entry of a copy for the first of n ascending positions (null: 0 .. n - 1), as a
-    // run or as blocks with masks: *taken positions in *units blocks; null when the
+    // An entry of a copy for the first of n ascending positions (null: p0 .. p0 + n - 1),
+    // as a run or as blocks with masks: *taken positions in *units blocks; null when the
     // table is full.  Runs of two blocks' length or more get entries of their own.
-    uint32_t *add_units(const int32_t *pos, int n, int unit0, int *taken, int *units) {
+    uint32_t *add_units(const int32_t *pos, int p0, int n, int unit0, int *taken, int *units) {
         const int room = tail - (docs + 1) * PK_ENTRY;
         if (room < 0) return nullptr;
         auto run = [&](int i) {
@@ -574,7 +574,8 @@ struct TableFill {
             while (j < n && pos[j] == pos[j - 1] + 1) ++j;
             return j - i;
         };
-        const int p0 = pos ? pos[0] : 0, k = pos ? run(0) : n;
+        if (pos) p0 = pos[0];
+        const int k = pos ? run(0) : n;
         uint32_t *e = entry(docs);
         e[PKC_UNIT0] = (uint32_t)unit0;
         e[PKE_POS] = (uint32_t)p0;
@@ -695,7 +696,10 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
             int keys = 0;
             for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
             const int ns = std::max(1, (int)((pk_blocks(keys) + range - 1) / range));
-            long long fit = q.n;
+            Tables::PackedLaunch &at = out.back();
+            long long fit = std::max<long long>(PK_MAX_GRID / Hkv - at.n_items, 0) / ns * cols / G;
+            if (at.n_items == 0) fit = std::max<long long>(fit, 1);  // (a row of many column groups, a small grid)
+            fit = std::min<long long>(fit, q.n);
             if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);
             const int before = fill.docs;
             const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, false, row_table);
@@ -1771,7 +1775,8 @@ static kvr_status copy_packed(kvr_ctx *c, const char *name, const kvr_pack_doc *
         const kvr_pack_doc &dc = docs[i];
         for (int done = 0; done < dc.n_positions;) {
             int n = 0, added = 0;
-            uint32_t *e = fill.add_units(dc.h_positions ? dc.h_positions + done : nullptr, dc.n_positions - done, units, &n, &added);
+            const int most = std::min(dc.n_positions - done, PK_MAX_GRID * PK_BLOCK);
+            uint32_t *e = units >= PK_MAX_GRID ? nullptr : fill.add_units(dc.h_positions ? dc.h_positions + done : nullptr, done, most, units, &n, &added);
             if (!e) {
                 const hipError_t err = flush();
                 if (err != hipSuccess) return hip_fail(c, err, name);
@@ -1858,7 +1863,8 @@ static kvr_status append_packed(kvr_ctx *c, int32_t layer, int32_t bits, const k
     for (int i = 0; i < n_docs; ++i) {
         const kvr_packed_rows &dc = docs[i];
         for (int done = 0; done < dc.n_rows;) {
-            const int n = fill.add(dc.d_packed, pk_blocks(dc.n_cap), row, dc.h_positions + done, 1, dc.n_rows - done, true, false);
+            const int most = std::min(dc.n_rows - done, PK_MAX_GRID - (row - first));
+            const int n = most < 1 ? 0 : fill.add(dc.d_packed, pk_blocks(dc.n_cap), row, dc.h_positions + done, 1, most, true, false);
             if (n == 0) {
                 const hipError_t e = flush();
                 if (e != hipSuccess) return hip_fail(c, e, who);

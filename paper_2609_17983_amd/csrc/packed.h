@@ -86,6 +86,9 @@ enum {
     PKC_RUN = 10,
 };
 constexpr uint32_t PK_RUN = 0xffffffffu, PK_ROWS = 0xfffffffeu;
+// Blocks (attention), rows (append) and units (copies) of a launch at most: enough to
+// fill a device many times, and far from the limits of a grid.
+constexpr int PK_MAX_GRID = 1 << 17;
 
 // Quantise the listed rows of k and v ([rows][stride] values, heads side by side)
 // into one layer's planes of the entries' packed caches.

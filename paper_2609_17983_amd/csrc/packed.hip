@@ -198,15 +198,16 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
 }
 
 template <typename T, int HP, int BITS, bool UNPACK>
-__global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_docs, int n_units, int hd, int Hkv) {
+__global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_docs, int n_units, int hd, int Hkv, int plane0) {
     constexpr int GS = HP / PK_GROUP, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
     constexpr int TPR = HP / 16, TPU = PK_BLOCK * TPR, NU = 256 / TPU;  // lanes of a row, of a unit; units
     __shared__ __attribute__((aligned(16))) char lds[NU][BB];
     const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPU), lt = threadIdx.x % TPU;
     const int r = lt / TPR, j = lt % TPR, d0 = 32 * (j >> 1) + 8 * (j & 1);
     const int unit = min((int)blockIdx.x * NU + sub, n_units - 1);  // a last odd one is done twice, alike
-    const PackedUnit u = pk_unit(t, n_docs, unit, blockIdx.y, BB);
-    const bool value = blockIdx.y / Hkv & 1, vec = hd % 8 == 0, mine = u.mask >> r & 1;
+    const int plane = plane0 + blockIdx.y;
+    const PackedUnit u = pk_unit(t, n_docs, unit, plane, BB);
+    const bool value = plane / Hkv & 1, vec = hd % 8 == 0, mine = u.mask >> r & 1;
     T *row = (T *)pk_pointer(u.e + PKC_CACHE) + (u.row + r) * hd;
     char *b = lds[sub];
     uint32_t *words = reinterpret_cast<uint32_t *>(b);
@@ -419,19 +420,22 @@ hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTabl
     if (n_units <= 0) return hipSuccess;
     if (n_docs < 1 || n_docs > PK_MAX_DOCS || hd > 128 || (bits != 4 && bits != 8)) return hipErrorInvalidValue;
     const int units = pk_width(hd) == 64 ? 2 : 1;
-    const dim3 grid((n_units + units - 1) / units, planes);
-#define KVR_CALL(HP, BITS)                                                                                             \
-    if (bf16 && unpack)                                                                                                \
-        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv);  \
-    else if (bf16)                                                                                                     \
-        kvr_launch((packed_copy_kernel<bf16_t, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv); \
-    else if (unpack)                                                                                                   \
-        kvr_launch((packed_copy_kernel<float, HP, BITS, true>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv);   \
-    else                                                                                                               \
-        kvr_launch((packed_copy_kernel<float, HP, BITS, false>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv)
-    KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
+    for (int p0 = 0; p0 < planes; p0 += 32768) {
+        const dim3 grid((n_units + units - 1) / units, std::min(planes - p0, 32768));
+#define KVR_COPY(T, HP, BITS, UN) \
+    kvr_launch((packed_copy_kernel<T, HP, BITS, UN>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv, p0)
+#define KVR_CALL(HP, BITS)                                   \
+    if (bf16 && unpack) KVR_COPY(bf16_t, HP, BITS, true);    \
+    else if (bf16) KVR_COPY(bf16_t, HP, BITS, false);        \
+    else if (unpack) KVR_COPY(float, HP, BITS, true);        \
+    else KVR_COPY(float, HP, BITS, false)
+        KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
 #undef KVR_CALL
-    return hipGetLastError();
+#undef KVR_COPY
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_rope_pack(bool bf16, int bits, const float *qkv, int nsplit, const void *bq, const void *bk,
