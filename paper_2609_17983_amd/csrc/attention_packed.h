@@ -83,6 +83,18 @@ __device__ __forceinline__ float pk_ror(float v) {
     return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x120 + N, 0xf, 0xf, true));
 }
 
+// The least and the largest value over a tile's 16 columns, for the whole wavefront.
+__device__ __forceinline__ void pk_minmax16(int *least, int *top) {
+    int lo = *least, hi = *top;
+#define KVR_STEP(N)                                                            \
+    lo = min(lo, __builtin_amdgcn_mov_dpp(lo, 0x120 + N, 0xf, 0xf, true));     \
+    hi = max(hi, __builtin_amdgcn_mov_dpp(hi, 0x120 + N, 0xf, 0xf, true));
+    KVR_STEP(8) KVR_STEP(4) KVR_STEP(2) KVR_STEP(1)
+#undef KVR_STEP
+    *least = __builtin_amdgcn_readfirstlane(lo);
+    *top = __builtin_amdgcn_readfirstlane(hi);
+}
+
 // Weight of a partial state with maximum m in one with maximum `all`.  A state
 // without a maximum is empty (zeros) or saw scores of NaN only, which stay.
 __device__ __forceinline__ float pk_weight(float m, float all) {
@@ -260,13 +272,11 @@ __device__ __forceinline__ void pk_query(const PackedAttnArgs &a, int64_t row, i
             for (int x = 0; x < QP; ++x)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    u[x][s] = u32x4{0, 0, 0, 0};
-                    for (int j = 0; j < 8; ++j) {
-                        const int d = 32 * s + 8 * g4 + j;
-                        const uint32_t v = d < a.hd ? (uint32_t)(x ? (const T *)a.q_lo + q0 : q)[d] : 0;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k == j >> 1) u[x][s][k] |= v << (16 * (j & 1));
+                    for (int j = 0; j < 4; ++j) {
+                        const int d = 32 * s + 8 * g4 + 2 * j;  // (hd is even)
+                        const T *p = (x ? (const T *)a.q_lo + q0 : q) + min(d, a.hd - 2);
+                        u[x][s][j] = d < a.hd ? (uint32_t)p[0] | ((uint32_t)p[1] << 16) : 0;
                     }
                 }
         }
@@ -284,7 +294,18 @@ __device__ __forceinline__ void pk_query(const PackedAttnArgs &a, int64_t row, i
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[s][j] = (float)q[min(32 * s + 8 * g4 + j, a.hd - 1)];
+            for (int j = 0; j < 8; ++j)
+                if (!q_vec) v[s][j] = (float)q[min(32 * s + 8 * g4 + j, a.hd - 1)];
+        if (q_vec) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f32x4 u = *reinterpret_cast<const f32x4 *>(q + min(32 * s + 8 * g4, a.hd - 8) + 4 * k);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[s][4 * k + j] = u[j];
+                }
+        }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
 #pragma unroll
@@ -303,15 +324,15 @@ __device__ __forceinline__ void pk_query(const PackedAttnArgs &a, int64_t row, i
 // T: the model's type.  QP: bf16 pieces of a query; CL: copies of the columns in a
 // tile.
 template <typename T, int HP, int BITS, int QP, int CL>
-__global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedTable t, PackedAttnArgs a, int cw,
-                                                                            int q_vec, int o_vec) {
+__global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedAttnArgs a, PackedTable t) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16;
     constexpr int PP = sizeof(T) == 4 ? 3 : 2;  // bf16 pieces of a probability times a scale
     constexpr bool CENTRED = sizeof(T) == 4;
     constexpr float RAW = BITS == 4 ? 16.f : 0.f;                      // a loaded code's offset
     constexpr float OFF = !CENTRED ? RAW : BITS == 4 ? -8.f : -128.f;  // the operand's
     constexpr int BB = pk_block_bytes(HP, BITS);
-    constexpr int ST = DT * 4 + 2;  // a lane's state per tile: O, m, l
+    constexpr int STATE = DT * 256 + 128;  // floats of a wavefront's state: O, then m and l
+    constexpr int CC_LOG = CL == 4 ? 2 : CL == 2 ? 3 : 4;
     // a step takes SB blocks of keys: TT key tiles, H of them for each copy
     constexpr int SB = CL == 4 ? 2 : 1, TT = 2 * SB, H = TT / CL, CC = 16 / CL;
     extern __shared__ float merge[];
@@ -319,17 +340,20 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int copy = (lane & 15) / CC, col = (lane & 15) % CC;
     // kv heads first: the longest items of all of them start before the shorter ones
-    const int kvh = blockIdx.x % a.Hkv, index = blockIdx.x / a.Hkv;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, index) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = index - (int)e[PKE_ITEM0];
-    const int cols = CC * cw;
-    const int kw = (int)(blockDim.x >> 6) / cw, wk = w / cw, wc = w - wk * cw;
-    const int split = nsplit == 1 ? 0 : item % nsplit;
+    const int kvh = blockIdx.x;
+    const PackedEntry e = pk_entry(t, a.n_docs, PKE_ITEM0, blockIdx.y);
+    const int nsplit = e.splits, item = (int)blockIdx.y - e.item0;
+    const int cw = 1 << a.cw_log, cols_log = CC_LOG + a.cw_log, cols = 1 << cols_log;
+    const int kw = 1 << (a.waves_log - a.cw_log), wk = w >> a.cw_log, wc = w & (cw - 1);
+    const int G = a.G, ncols_doc = e.rows * G;
+    // column groups from the last one down: later rows see more keys
+    const int ncg = (ncols_doc + cols - 1) >> cols_log;
+    const int down = nsplit == 1 ? item : ncg == 1 ? 0 : item / nsplit, split = item - down * nsplit, cg = ncg - 1 - down;
     // the first blocks' loads wait for nothing else
-    const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
-    const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
+    const size_t plane = (size_t)e.blocks * BB;
+    const char *kp = e.packed + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
     const char *vp = kp + a.Hkv * plane;
-    const int last = (int)e[PKE_BLOCKS] - 1;
+    const int last = e.blocks - 1;
     PackedBlock<HP, BITS> kb[SB], vb[SB];
     u32x4 kpar[H][GS], vpar[H][GS];  // of this lane's keys
     // Blocks b .. b + SB - 1; an odd document's last step loads its last block twice.
@@ -348,34 +372,25 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     const int b0 = split * (a.range / PK_BLOCK) + wk * SB;
     load_keys(min(b0, last));
     load_values(min(b0, last));
-    const int G = a.Hq / a.Hkv, ncols_doc = (int)e[PKE_ROWS] * G;
-    // column groups from the last one down: later rows see more keys
-    const int ncg = (ncols_doc + cols - 1) / cols;
-    const int cg = ncg - 1 - (nsplit == 1 ? item : item / nsplit);
-    const int row0 = e[PKE_ROW0];
+    const int row0 = e.row0;
 
     // this lane's column: its row, head and number of visible keys
     const int column = cg * cols + wc * CC + col;
     const bool valid = column < ncols_doc;
     const int row = valid ? column / G : 0, head = kvh * G + (valid ? column - row * G : 0);
-    const int limit = valid ? min(pk_position(t, e, row, a.rows) + 1, (int)e[PKE_KEYS]) : 0;
+    const int limit = valid ? min(pk_position(t, e, row, a.rows) + 1, e.keys) : 0;
     bf16x8 qv[QP][KS];
     float qsum[GS];
-    pk_query<T, HP, QP>(a, row0 + row, head, g4, q_vec, qv, qsum);
+    pk_query<T, HP, QP>(a, row0 + row, head, g4, a.q_vec, qv, qsum);
     int top = limit, least = valid ? limit : 0x7fffffff;
 #pragma unroll
     for (int g = 0; g < GS; ++g) qsum[g] = pk_sum4(qsum[g]);
     // the wavefront's last visible key, and the keys that all its columns see
-#pragma unroll
-    for (int o = 1; o < CC; o *= 2) {
-        top = max(top, __shfl_xor(top, o, 64));
-        least = min(least, __shfl_xor(least, o, 64));
-    }
-    top = __builtin_amdgcn_readfirstlane(top);
-    least = __builtin_amdgcn_readfirstlane(least);
+    pk_minmax16(&least, &top);
     const int b1 = (min(top, (split + 1) * a.range) + PK_BLOCK - 1) / PK_BLOCK;
-    // steps that begin before it need no mask
-    const int b_full = min(b1, least / PK_BLOCK) - (SB - 1);
+    // Steps that begin before it need no mask.  With copies there are few values to mask:
+    // one loop for all (5 % of its instructions are the masks), half the code.
+    const int b_full = CL > 1 ? 0 : min(b1, least / PK_BLOCK) - (SB - 1);
 
     f32x4 o[DT];
     float m = -INFINITY, l = 0.f, z[GS];
@@ -383,7 +398,7 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int g = 0; g < GS; ++g) z[g] = 0.f;
-    const float sc = 1.4426950408889634f / sqrtf((float)a.hd);
+    const float sc = a.scale;
     uint32_t mine[CL];  // all ones for this lane's copy
 #pragma unroll
     for (int c = 0; c < CL; ++c) mine[c] = copy == c ? 0xffffffffu : 0u;
@@ -512,8 +527,10 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
         if (more) load_values(b + kw * SB);
     };
     int b = b0;
+    if constexpr (CL == 1) {
 #pragma unroll 1
-    for (; b < b_full; b += kw * SB) step(b, std::false_type{});
+        for (; b < b_full; b += kw * SB) step(b, std::false_type{});
+    }
 #pragma unroll 1
     for (; b < b1; b += kw * SB) step(b, std::true_type{});
 
@@ -543,42 +560,39 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     // Lane: one column, dimensions 16 d + 4 g4 + i.  The wavefronts of a tile hand their
     // states to each other through LDS, and wavefront wk finishes the dimension tiles wk,
     // wk + kw, ..
-    float *const mg = merge + (size_t)wc * ST * 64 + lane;
-    const int mstep = cw * ST * 64;
-    float *own = mg + wk * mstep;
+    float *const own = merge + (size_t)(wk * cw + wc) * STATE;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) own[(d * 4 + i) * 64] = o[d][i];
-    own[DT * 4 * 64] = m;
-    own[(DT * 4 + 1) * 64] = l;
+    for (int d = 0; d < DT; ++d) reinterpret_cast<f32x4 *>(own)[d * 64 + lane] = o[d];
+    reinterpret_cast<f32x2 *>(own + DT * 256)[lane] = f32x2{m, l};
     __syncthreads();
     if (!valid || copy > 0) return;
-    const float *p = mg;
-    float all = -INFINITY, sum = 0.f, f[PK_WAVES_MAX];
+    const float *const first = merge + (size_t)wc * STATE;
+    const int next = cw * STATE;  // from a wavefront of the tile to the next
+    float all = -INFINITY, sum = 0.f, f[PK_WAVES_MAX], ls[PK_WAVES_MAX];
 #pragma unroll
-    for (int k = 0; k < PK_WAVES_MAX; ++k) f[k] = k < kw ? p[k * mstep + DT * 4 * 64] : -INFINITY;
+    for (int k = 0; k < PK_WAVES_MAX; ++k) {
+        const f32x2 ml = k < kw ? reinterpret_cast<const f32x2 *>(first + k * next + DT * 256)[lane] : f32x2{-INFINITY, 0.f};
+        f[k] = ml[0];
+        ls[k] = ml[1];
+    }
 #pragma unroll
     for (int k = 0; k < PK_WAVES_MAX; ++k) all = fmaxf(all, f[k]);
 #pragma unroll
     for (int k = 0; k < PK_WAVES_MAX; ++k) {
         f[k] = pk_weight(f[k], all);
-        if (k < kw) sum += p[k * mstep + (DT * 4 + 1) * 64] * f[k];
+        sum += ls[k] * f[k];
     }
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    float *part = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * cols + wc * CC + col) * (HP + 4);
+    float *part = a.part + (((size_t)(e.part0 + cg * nsplit + split) * a.Hkv + kvh) * cols + wc * CC + col) * (HP + 4);
 #pragma unroll 1
     for (int d = wk; d < DT; d += kw) {
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < PK_WAVES_MAX; ++k)
-            if (k < kw) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] += p[k * mstep + (d * 4 + i) * 64] * f[k];
-            }
+            if (k < kw) y += reinterpret_cast<const f32x4 *>(first + k * next)[d * 64 + lane] * f[k];
         const int dim = 16 * d + 4 * g4;
         if (nsplit > 1) *reinterpret_cast<f32x4 *>(part + dim) = y;
-        else if (dim < a.hd) pk_store<T>(a, row0 + row, head * a.hd + dim, min(4, a.hd - dim), o_vec, y * inv);
+        else if (dim < a.hd) pk_store<T>(a, row0 + row, head * a.hd + dim, min(4, a.hd - dim), a.o_vec, y * inv);
     }
     if (nsplit > 1 && g4 == 0 && wk == 0) {
         part[HP] = all;
@@ -586,48 +600,49 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
     }
 }
 
-// Whether query and output rows can be moved in 16-byte (output, bf16: 8-byte) pieces.
-inline void pk_vectors(bool bf16, const PackedAttnArgs &a, bool *q_vec, bool *o_vec) {
+inline int pk_log(int x) { return 31 - __builtin_clz(x); }  // of a power of two
+
+// The arguments with what the launchers add.  Query and output rows can be moved in
+// vectors where every row's pieces are aligned (16 bytes; bf16 outputs 8).
+inline PackedAttnArgs pk_complete(bool bf16, PackedShape sh, PackedAttnArgs a) {
     const size_t es = bf16 ? 2 : 4;
     auto aligned = [](const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; };
-    *q_vec = bf16 && a.hd % 8 == 0 && a.q_stride % 8 == 0 && aligned(a.q, 16) && aligned(a.q_lo, 16);
-    *o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && aligned(a.out, 4 * es) && aligned(a.out_lo, 4 * es);
+    a.q_vec = a.hd % 8 == 0 && a.q_stride % (16 / es) == 0 && aligned(a.q, 16) && aligned(a.q_lo, 16);
+    a.o_vec = a.hd % 4 == 0 && a.out_stride % 4 == 0 && aligned(a.out, 4 * es) && aligned(a.out_lo, 4 * es);
+    a.G = a.Hkv > 0 ? a.Hq / a.Hkv : 1;
+    a.scale = 1.4426950408889634f / sqrtf((float)a.hd);
+    a.waves_log = pk_log(sh.waves);
+    a.cw_log = pk_log(sh.cw);
+    return a;
 }
 
 template <typename T, int HP, int BITS, int QP, int CL>
-hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec, hipStream_t s,
-                     int *resident) {
-    const uint32_t lds = (uint32_t)sh.waves * (HP / 4 + 2) * 64 * 4;  // the wavefronts' states
+hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, hipStream_t s, int *resident) {
+    const uint32_t lds = (uint32_t)sh.waves * (HP / 16 * 256 + 128) * 4;  // the wavefronts' states
     static std::atomic<int> known[2];
     if (resident) return pk_resident(attention_packed_kernel<T, HP, BITS, QP, CL>, sh.waves, lds, known, resident);
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.n_items * a.Hkv), dim3(64 * sh.waves), lds, s, t, a,
-               sh.cw, (int)q_vec, (int)o_vec);
+    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, a, t);
     return hipGetLastError();
 }
 
 template <typename T, int HP, int BITS, int QP>
-hipError_t pk_launch_copies(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, bool q_vec, bool o_vec,
-                            hipStream_t s, int *resident) {
-    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 4>(t, a, sh, q_vec, o_vec, s, resident);
-    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 2>(t, a, sh, q_vec, o_vec, s, resident);
-    return pk_launch<T, HP, BITS, QP, 1>(t, a, sh, q_vec, o_vec, s, resident);
+hipError_t pk_launch_copies(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, hipStream_t s, int *resident) {
+    if (sh.copies == 4) return pk_launch<T, HP, BITS, QP, 4>(t, a, sh, s, resident);
+    if (sh.copies == 2) return pk_launch<T, HP, BITS, QP, 2>(t, a, sh, s, resident);
+    return pk_launch<T, HP, BITS, QP, 1>(t, a, sh, s, resident);
 }
 
 template <int HP, int BITS>
-hipError_t pk_launch_bits(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, bool q_vec, bool o_vec,
-                          hipStream_t s, int *resident) {
-    if (!bf16) return pk_launch_copies<float, HP, BITS, 3>(t, a, sh, q_vec, o_vec, s, resident);
-    return a.q_lo ? pk_launch_copies<bf16_t, HP, BITS, 2>(t, a, sh, q_vec, o_vec, s, resident)
-                  : pk_launch_copies<bf16_t, HP, BITS, 1>(t, a, sh, q_vec, o_vec, s, resident);
+hipError_t pk_launch_bits(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident) {
+    if (!bf16) return pk_launch_copies<float, HP, BITS, 3>(t, a, sh, s, resident);
+    return a.q_lo ? pk_launch_copies<bf16_t, HP, BITS, 2>(t, a, sh, s, resident)
+                  : pk_launch_copies<bf16_t, HP, BITS, 1>(t, a, sh, s, resident);
 }
 
 template <int HP>
 hipError_t pk_launch_width(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s,
                            int *resident) {
-    bool q_vec, o_vec;
-    pk_vectors(bf16, a, &q_vec, &o_vec);
-    return bits == 4 ? pk_launch_bits<HP, 4>(bf16, sh, t, a, q_vec, o_vec, s, resident)
-                     : pk_launch_bits<HP, 8>(bf16, sh, t, a, q_vec, o_vec, s, resident);
+    return bits == 4 ? pk_launch_bits<HP, 4>(bf16, sh, t, a, s, resident) : pk_launch_bits<HP, 8>(bf16, sh, t, a, s, resident);
 }
 
 }  // namespace

@@ -12,21 +12,21 @@ namespace {
 // WC wavefronts take WC * 256 / HP ranges at a time, UN of them in flight, each group
 // keeps a running maximum, and the groups are joined through LDS.
 template <typename T, int HP, int WC>
-__global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedTable t, PackedAttnArgs a, int cols, int o_vec) {
+__global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedAttnArgs a, PackedTable t, int cols_log) {
     constexpr int L = HP / 4, GR = 64 / L, UN = 4;
     __shared__ float red[4][64][6];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kvh = blockIdx.y;
     const int x = blockIdx.x * (4 / WC) + w / WC;  // column of the launch
-    const int cgx = min(x / cols, a.n_cg - 1), cc = x % cols;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_CG0, cgx) * PK_ENTRY;
-    const int G = a.Hq / a.Hkv, c = (cgx - (int)e[PKE_CG0]) * cols + cc;
-    const int ns = x / cols < a.n_cg && c < (int)e[PKE_ROWS] * G ? (int)e[PKE_SPLITS] : 1;
+    const int cols = 1 << cols_log, cgx = min(x >> cols_log, a.n_cg - 1), cc = x & (cols - 1);
+    const PackedEntry e = pk_entry(t, a.n_docs, PKE_CG0, cgx);
+    const int G = a.G, c = (cgx - e.cg0) * cols + cc;
+    const int ns = x >> cols_log < a.n_cg && c < e.rows * G ? e.splits : 1;
     // (the same for all wavefronts of a column; with WC > 1 of the block)
     float m = -INFINITY, l = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     if (ns > 1) {
         const size_t step = (size_t)a.Hkv * cols * (HP + 4);
-        const float *p = a.part + (((size_t)((int)e[PKE_PART0] + (cgx - (int)e[PKE_CG0]) * ns) * a.Hkv + kvh) * cols + cc) * (HP + 4);
+        const float *p = a.part + (((size_t)(e.part0 + (cgx - e.cg0) * ns) * a.Hkv + kvh) * cols + cc) * (HP + 4);
         const int d = (lane % L) * 4, first = (w % WC) * GR + lane / L;
         for (int i0 = first; i0 < ns; i0 += UN * WC * GR) {
             f32x4 v[UN];
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedTab
     const int d = (lane % L) * 4;
     if (ns <= 1 || lane >= L || d >= a.hd) return;
     const int r = c / G, h = kvh * G + c - r * G;
-    pk_store<T>(a, (int64_t)e[PKE_ROW0] + r, h * a.hd + d, min(4, a.hd - d), o_vec, y * (l == 0.f ? 0.f : 1.0f / l));
+    pk_store<T>(a, (int64_t)e.row0 + r, h * a.hd + d, min(4, a.hd - d), a.o_vec, y * (l == 0.f ? 0.f : 1.0f / l));
 }
 
 }  // namespace
@@ -88,8 +88,9 @@ hipError_t launch_attention_packed64(bool bf16, int bits, PackedShape sh, const 
                                      hipStream_t s, int *resident);
 hipError_t launch_attention_packed_rows(int bits, const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident);
 
-hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
+hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &args,
                                    hipStream_t s, int *resident) {
+    const PackedAttnArgs a = pk_complete(bf16, sh, args);
     if (!resident && a.n_items <= 0) return hipSuccess;
     if (a.hd > 128 || (bits != 4 && bits != 8) || (!resident && a.n_docs < 1) || a.n_docs > PK_MAX_DOCS || a.range % PK_BLOCK != 0)
         return hipErrorInvalidValue;
@@ -103,17 +104,16 @@ hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const Pa
                                 : pk_launch_width<128>(bf16, bits, sh, t, a, s, resident);
 }
 
-hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
+hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const PackedTable &t, const PackedAttnArgs &args,
                                            hipStream_t s) {
-    const int cols = pk_cols(sh);
-    bool q_vec, o_vec;
-    pk_vectors(bf16, a, &q_vec, &o_vec);
+    const int cols = pk_cols(sh), cols_log = pk_log(cols);
+    const PackedAttnArgs a = pk_complete(bf16, sh, args);
     const int wc = a.max_splits > 8 ? 4 : 1;
     const dim3 grid((unsigned)(((size_t)a.n_cg * cols * wc + 3) / 4), a.Hkv);
 #define KVR_COMBINE(T, HP)                                                                                                    \
     do {                                                                                                                      \
-        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, t, a, cols, (int)o_vec);       \
-        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, t, a, cols, (int)o_vec);               \
+        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, a, t, cols_log);       \
+        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, a, t, cols_log);               \
     } while (0)
     if (pk_width(a.hd) == 64) {
         if (bf16) KVR_COMBINE(bf16_t, 64);

@@ -30,8 +30,7 @@ __device__ __forceinline__ void pr_split(const float v[8], u32x4 *hi, u32x4 *lo)
 }
 
 template <int HP, int BITS, int QP>
-__global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(PackedTable t, PackedAttnArgs a, int q_vec,
-                                                                             int o_vec) {
+__global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(PackedAttnArgs a, PackedTable t) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
     constexpr int NT = PR_TILES, COLS = pk_cols(PACKED_ROWS);
     // operands of a key block: keys [16-key tile][step][lane], values [16-dimension tile][lane]
@@ -43,14 +42,14 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
 
     const int lane = threadIdx.x & 63, g4 = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // kv heads first: the longest items of all of them start before the shorter ones
-    const int kvh = blockIdx.x % a.Hkv, index = blockIdx.x / a.Hkv;
-    const uint32_t *e = t.w + pk_find(t, a.n_docs, PKE_ITEM0, index) * PK_ENTRY;
-    const int nsplit = e[PKE_SPLITS], item = index - (int)e[PKE_ITEM0];
+    const int kvh = blockIdx.x;
+    const PackedEntry e = pk_entry(t, a.n_docs, PKE_ITEM0, blockIdx.y);
+    const int nsplit = e.splits, item = (int)blockIdx.y - e.item0;
     const int split = nsplit == 1 ? 0 : item % nsplit;
-    const size_t plane = (size_t)e[PKE_BLOCKS] * BB;
-    const char *kp = pk_pointer(e) + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
+    const size_t plane = (size_t)e.blocks * BB;
+    const char *kp = e.packed + ((size_t)a.layer * 2 * a.Hkv + kvh) * plane;
     const char *vp = kp + a.Hkv * plane;
-    const int last = (int)e[PKE_BLOCKS] - 1, keys = e[PKE_KEYS];
+    const int last = e.blocks - 1, keys = e.keys;
     const int b0 = split * (a.range / PK_BLOCK);
 
     // A thread's units of a block: wavefront w makes key operand w and value operand w
@@ -135,11 +134,11 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     };
     fetch(min(b0, last));
 
-    const int G = a.Hq / a.Hkv, ncols_doc = (int)e[PKE_ROWS] * G;
+    const int G = a.G, ncols_doc = e.rows * G;
     // column groups from the last one down: later rows see more keys
     const int ncg = (ncols_doc + COLS - 1) / COLS;
     const int cg = ncg - 1 - (nsplit == 1 ? item : item / nsplit);
-    const int row0 = e[PKE_ROW0];
+    const int row0 = e.row0;
     int row[NT], head[NT], limit[NT];
     bool valid[NT];
     bf16x8 qv[NT][QP][KS];
@@ -152,17 +151,11 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
         head[n] = kvh * G + (valid[n] ? c - row[n] * G : 0);
         limit[n] = valid[n] ? min(pk_position(t, e, row[n], a.rows) + 1, keys) : 0;
         float unused[GS];
-        pk_query<bf16_t, HP, QP>(a, row0 + row[n], head[n], g4, q_vec, qv[n], unused);
+        pk_query<bf16_t, HP, QP>(a, row0 + row[n], head[n], g4, a.q_vec, qv[n], unused);
         top = max(top, limit[n]);
         if (valid[n]) least = min(least, limit[n]);
     }
-#pragma unroll
-    for (int o = 1; o < 16; o *= 2) {
-        top = max(top, __shfl_xor(top, o, 64));
-        least = min(least, __shfl_xor(least, o, 64));
-    }
-    top = __builtin_amdgcn_readfirstlane(top);
-    least = __builtin_amdgcn_readfirstlane(least);
+    pk_minmax16(&least, &top);
     // the block's last key: the largest of its wavefronts'
     int *const tops = flags + 4;
     if (lane == 0) tops[w] = top;
@@ -184,7 +177,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
         m[n] = -INFINITY;
         l[n] = 0.f;
     }
-    const float sc = 1.4426950408889634f / sqrtf((float)a.hd);
+    const float sc = a.scale;
     if (b0 < b1) {
         stage(b0, 0);
         if (b0 + 1 < b1) fetch(b0 + 1);
@@ -296,13 +289,13 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
         const float sum = pk_sum4(l[n]);
         if (!valid[n]) continue;
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        float *part = a.part + (((size_t)((int)e[PKE_PART0] + cg * nsplit + split) * a.Hkv + kvh) * COLS +
+        float *part = a.part + (((size_t)(e.part0 + cg * nsplit + split) * a.Hkv + kvh) * COLS +
                                 (w * NT + n) * 16 + (lane & 15)) * (HP + 4);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const int dim = 16 * d + 4 * g4;
             if (nsplit > 1) *reinterpret_cast<f32x4 *>(part + dim) = o[n][d];
-            else if (dim < a.hd) pk_store<bf16_t>(a, row0 + row[n], head[n] * a.hd + dim, min(4, a.hd - dim), o_vec, o[n][d] * inv);
+            else if (dim < a.hd) pk_store<bf16_t>(a, row0 + row[n], head[n] * a.hd + dim, min(4, a.hd - dim), a.o_vec, o[n][d] * inv);
         }
         if (nsplit > 1 && g4 == 0) {
             part[HP] = m[n];
@@ -313,16 +306,14 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
 
 template <int HP, int BITS>
 hipError_t pr_launch(const PackedTable &t, const PackedAttnArgs &a, hipStream_t s, int *resident) {
-    bool q_vec, o_vec;
-    pk_vectors(true, a, &q_vec, &o_vec);
-    const dim3 grid(a.n_items * a.Hkv), block(64 * PR_WAVES);
+    const dim3 grid(a.Hkv, a.n_items), block(64 * PR_WAVES);
     const uint32_t bytes = 2 * 2 * (HP / 8) * 64 * 16 + (4 + PR_WAVES) * 4;
     static std::atomic<int> known[2][2];
     if (resident)
         return a.q_lo ? pk_resident(attention_packed_rows_kernel<HP, BITS, 2>, PR_WAVES, bytes, known[1], resident)
                       : pk_resident(attention_packed_rows_kernel<HP, BITS, 1>, PR_WAVES, bytes, known[0], resident);
-    if (a.q_lo) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
-    else kvr_launch((attention_packed_rows_kernel<HP, BITS, 1>), grid, block, bytes, s, t, a, (int)q_vec, (int)o_vec);
+    if (a.q_lo) kvr_launch((attention_packed_rows_kernel<HP, BITS, 2>), grid, block, bytes, s, a, t);
+    else kvr_launch((attention_packed_rows_kernel<HP, BITS, 1>), grid, block, bytes, s, a, t);
     return hipGetLastError();
 }
 

@@ -655,8 +655,9 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
     // Key ranges: as many blocks as the device holds at a time and no more, so that none
     // waits for a second round (us a call, with as many blocks and with half as many
     // again: 64 documents of 2000-8000 positions, 32 heads, 80 and 98; 60 documents, 28
-    // heads, 48 and 55; 8 documents of 48 rows 57 and 94), and two steps a wavefront at
-    // least.  Little work takes blocks of eight wavefronts, whose partials are fewer (one
+    // heads, 48 and 55; 8 documents of 48 rows 57 and 94).  Two
+    // steps a wavefront are not worth a split (512 positions, 8.4 us a call in one and
+    // 11.5 in two).  Little work takes blocks of eight wavefronts, whose partials are fewer (one
     // document of 40001 positions 17.5, blocks of four 18.7); much work for few columns
     // blocks of four, which come out more even (64 documents 80 and 90).
     const bool large = most_cols <= 16 && units >= 6ll * 768 * 4 * sb;
@@ -669,8 +670,8 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
     const hipError_t err = launch_attention_packed(c->bf16, bits, sh, PackedTable{}, probe, nullptr, &target);
     if (err != hipSuccess) return err;
     const long long whole = (pk_blocks(std::max(longest, 1)) + sb - 1) / sb * sb;
-    long long range = std::max<long long>(2 * kw * sb, (units + target - 1) / target);
-    range = std::min(whole, (range + sb - 1) / sb * sb);
+    long long range = std::max<long long>(kw * sb, (units + target - 1) / target);
+    range = whole <= 2 * kw * sb ? whole : std::min(whole, (range + sb - 1) / sb * sb);
     while (range < whole && count(range) > target) range = std::min(whole, range + std::max<long long>(range / 16 / sb * sb, sb));
     const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
@@ -697,7 +698,7 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
             for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
             const int ns = std::max(1, (int)((pk_blocks(keys) + range - 1) / range));
             Tables::PackedLaunch &at = out.back();
-            long long fit = std::max<long long>(PK_MAX_GRID / Hkv - at.n_items, 0) / ns * cols / G;
+            long long fit = std::max<long long>(PK_MAX_GRID - at.n_items, 0) / ns * cols / G;
             if (at.n_items == 0) fit = std::max<long long>(fit, 1);  // (a row of many column groups, a small grid)
             fit = std::min<long long>(fit, q.n);
             if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);

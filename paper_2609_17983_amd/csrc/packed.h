@@ -56,7 +56,7 @@ __host__ __device__ __forceinline__ int pk_value_byte(int hp, int bits, int r, i
 constexpr int PK_WORDS = 896, PK_ENTRY = 12;
 constexpr int PK_MAX_DOCS = PK_WORDS / PK_ENTRY;
 struct PackedTable {
-    uint32_t w[PK_WORDS];
+    alignas(8) uint32_t w[PK_WORDS];
 };
 // Words of an entry.  Rows r of an entry are rows ROW0 + r of the launch's row
 // arrays; their positions are POS + r (POS >= 0 or -1) when REF is
@@ -88,7 +88,7 @@ enum {
 constexpr uint32_t PK_RUN = 0xffffffffu, PK_ROWS = 0xfffffffeu;
 // Blocks (attention), rows (append) and units (copies) of a launch at most: enough to
 // fill a device many times, and far from the limits of a grid.
-constexpr int PK_MAX_GRID = 1 << 17;
+constexpr int PK_MAX_GRID = 1 << 15;
 
 // Quantise the listed rows of k and v ([rows][stride] values, heads side by side)
 // into one layer's planes of the entries' packed caches.
@@ -116,6 +116,13 @@ struct PackedAttnArgs {
     int32_t n_docs, n_items, n_cg;
     int32_t range;          // keys of a key range (a multiple of a step's)
     int32_t max_splits;     // largest number of key ranges of a document
+    // set by the launchers (a block's start is latency: no divisions there that the host
+    // can make): Hq / Hkv, log2(e) / sqrt(hd), base-2 logarithms of a block's wavefronts
+    // and of its column tiles, and whether rows can be moved in vectors (pk_vectors)
+    int32_t G;
+    float scale;
+    int32_t waves_log, cw_log;
+    int32_t q_vec, o_vec;
 };
 // A block of `waves` wavefronts: cw of them hold a column tile each, with the columns
 // (row, query head of the kv head's group) `copies` times in it; the waves / cw
@@ -166,15 +173,32 @@ __device__ __forceinline__ int pk_find(const PackedTable &t, int n_docs, int wor
     for (int b = 0; b < B; ++b) n += __popcll(__ballot(b * 64 + lane < n_docs && v[b] <= x));
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
+// An attention entry, as its words stand in the table.
+struct PackedEntry {
+    const char *packed;
+    int32_t blocks, row0, rows;
+    uint32_t ref;
+    int32_t pos, item0, cg0, splits, part0, keys;
+};
+static_assert(sizeof(PackedEntry) == PK_ENTRY * 4, "entry words");
+// The entry that holds index x.  The first one is loaded with the arguments, so that
+// the usual launch of one document has no second round trip.
+__device__ __forceinline__ PackedEntry pk_entry(const PackedTable &t, int n_docs, int word, int x) {
+    PackedEntry e = *reinterpret_cast<const PackedEntry *>(t.w);
+    if (n_docs > 1) e = *reinterpret_cast<const PackedEntry *>(t.w + pk_find(t, n_docs, word, x) * PK_ENTRY);
+    return e;
+}
+__device__ __forceinline__ int pk_position(const PackedTable &t, const PackedEntry &e, int r, const RowInfo *rows) {
+    if (e.ref == PK_RUN) return e.pos + r;
+    if (e.ref == PK_ROWS) return rows[e.row0 + r].pos;
+    return (int)t.w[e.ref + r];
+}
 __device__ __forceinline__ char *pk_pointer(const uint32_t *e) {
     return (char *)(((uint64_t)e[1] << 32) | e[0]);
 }
-// Position of row r of entry e.
-__device__ __forceinline__ int pk_position(const PackedTable &t, const uint32_t *e, int r, const RowInfo *rows) {
-    const uint32_t ref = e[PKE_REF];
-    if (ref == PK_RUN) return (int)e[PKE_POS] + r;
-    if (ref == PK_ROWS) return rows[e[PKE_ROW0] + r].pos;
-    return (int)t.w[ref + r];
+// Position of row r of entry e of an append.
+__device__ __forceinline__ int pk_position(const PackedTable &t, const uint32_t *e, int r) {
+    return e[PKE_REF] == PK_RUN ? (int)e[PKE_POS] + r : (int)t.w[e[PKE_REF] + r];
 }
 #endif
 

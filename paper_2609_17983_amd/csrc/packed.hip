@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedTable t, int n
     const bool value = plane >= Hkv;
     const T *src = (value ? v : k) + (size_t)row * stride + (plane - (value ? Hkv : 0)) * hd;
     const float x[2] = {lane < hd ? to_f32(src[lane]) : 0.f, 64 + lane < hd ? to_f32(src[64 + lane]) : 0.f};
-    const int p = pk_position(t, e, row - (int)e[PKE_ROW0], nullptr);
+    const int p = pk_position(t, e, row - (int)e[PKE_ROW0]);
     constexpr int BB = pk_block_bytes(HP, BITS);
     char *base = pk_pointer(e) + (((size_t)layer * 2 * Hkv + plane) * e[PKE_BLOCKS] + p / PK_BLOCK) * BB;
     write_row<HP, BITS>(x, hd, value, base, p % PK_BLOCK);
