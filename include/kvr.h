@@ -362,10 +362,12 @@ kvr_status kvr_transplant(kvr_ctx *ctx, const void *d_src, int32_t src_n_cap, vo
  *     8 bits: byte ((l * (W/16) + d/16) * 2 + r/16) * 4 + r%4
  * (the order in which the matrix units take them; nibbles and bytes count from the
  * low end).  A packed cache is 16-byte aligned; kvr_packed_bytes() gives its size.
- * It needs no initialisation: what no call wrote is not read, except by a query row
+ * It needs no initialisation: what no call wrote has no effect, except on a query row
  * whose position is behind it.
  *
- * In the calls below `bits` other than 4 or 8 is KVR_E_UNSUPPORTED. */
+ * In the calls below `bits` other than 4 or 8 is KVR_E_UNSUPPORTED.  A cache does not
+ * say its bits or its dimensions: every call on it names those that it was written with,
+ * and its n_cap, at most 2^30 (KVR_E_RANGE). */
 
 /* Bytes of one document's packed cache, 0 for invalid arguments. */
 size_t kvr_packed_bytes(const kvr_dims *dims, int32_t n_cap, int32_t bits);
@@ -424,7 +426,11 @@ kvr_status kvr_append_packed(kvr_ctx *ctx, int32_t layer, int32_t bits, const kv
  * context's dtype, aligned to it, not overlapping) hold a row of n_heads * head_dim
  * values per listed row, q_stride and out_stride values apart (queries after the
  * rotary embedding).  Scores, softmax and sums are fp32; the products take the codes,
- * not rounded values.  Errors: KVR_E_ARG (NULL or misaligned pointers), KVR_E_RANGE
+ * not rounded values.  The sums hold cached values up to 2^96; larger ones may overflow
+ * there (an output that is not finite).  The kernel and the key ranges that a row gets
+ * depend on the call's other rows too: equal calls give equal results, a row in another
+ * batch the same to fp32 rounding (bf16 contexts: 2^-16 of the products), before its
+ * output is rounded.  Errors: KVR_E_ARG (NULL or misaligned pointers), KVR_E_RANGE
  * (layer, n_cap, a position, a stride below n_heads * head_dim, or more than
  * 2^31 - 1 rows times heads), KVR_E_UNSUPPORTED, KVR_E_NOMEM, KVR_E_HIP. */
 kvr_status kvr_attention_packed(kvr_ctx *ctx, int32_t layer, int32_t bits, const kvr_packed_rows *docs, int32_t n_docs,

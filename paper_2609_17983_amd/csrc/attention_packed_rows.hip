@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
         }
     };
     // The fetched block's operands into a buffer.
-    auto stage = [&](int b, int buf) {
+    auto stage = [&](int buf) {
         u32x4 *const base = lds + buf * BUF;
         if (has_key) {
             float v[8];
@@ -124,9 +124,6 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
                         v[j] = 0.f;
                         slots |= 1u << (16 * (j >> 2) + 4 * g4 + (j & 3));
                     }
-                // slots behind the last position that any row sees hold anything
-                const int seen = min(keys - b * PK_BLOCK, PK_BLOCK);
-                slots &= 0xffffffffu >> (32 - seen);
                 if (slots) atomicOr(&flags[buf * 2 + (GS > 1 ? vu / 4 : 0)], (int)slots);
             }
             pr_split(v, base + (KU + vu) * 64 + lane, base + (KU + VU + KU + vu) * 64 + lane);
@@ -179,7 +176,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
     }
     const float sc = a.scale;
     if (b0 < b1) {
-        stage(b0, 0);
+        stage(0);
         if (b0 + 1 < b1) fetch(b0 + 1);
     }
     for (int b = b0; b < b1; ++b) {
@@ -189,7 +186,7 @@ __global__ __launch_bounds__(64 * PR_WAVES) void attention_packed_rows_kernel(Pa
         // products, half after them: vector and matrix instructions then run side by side
         auto next = [&] {
             if (b + 1 < b1) {
-                stage(b + 1, buf ^ 1);
+                stage(buf ^ 1);
                 if (b + 2 < b1) fetch(b + 2);
             }
         };

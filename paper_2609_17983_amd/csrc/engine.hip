@@ -46,12 +46,12 @@ struct Tables {
     // packed caches: the launches of one layer's attention
     struct PackedLaunch {
         PackedTable table;
+        PackedShape sh;
+        int range;  // keys of a key range
         int n_docs, n_items, n_cg;
         int splits;  // largest number of key ranges
     };
     std::vector<PackedLaunch> packed;
-    PackedShape packed_shape{};
-    int packed_range = 0;
     int att_mt = 1;  // 16-row tiles per attention item (rows of a row block / 16)
     void clear() {
         rows.clear(); docs.clear(); items.clear(); comb.clear(); blocks.clear(); packed.clear();
@@ -585,7 +585,7 @@ struct TableFill {
             *taken = k;
             *units = (p0 + k - 1) / PK_BLOCK - p0 / PK_BLOCK + 1;
         } else {
-            // the pairs are written downwards from the tail: units in descending order of blocks
+            // the pairs are written downwards from the tail, the first block's last
             int m = 0, i = 0;
             while (i < n) {
                 if (pos[i] % PK_BLOCK == 0 && run(i) >= 2 * PK_BLOCK) break;
@@ -615,122 +615,215 @@ struct PackedQuery {
     const int32_t *pos;
     int step;
 };
+// What a plan looks at of a document: its columns, and the keys that a row sees at most
+// and on average.
+struct PackedSize {
+    long long cols;
+    int keys;
+    double mean;
+};
 
-// The attention launches of rows over packed caches (t.packed): which columns a
-// block takes, and into how many key ranges a document's keys are cut.  pair: the
-// queries are compensated pairs.
-template <typename DocAt>
-hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_docs, DocAt doc, bool row_table) {
-    const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
-    t.packed.clear();
-    // the documents' rows and keys
-    struct Size { long long cols; int blocks; };
-    std::vector<Size> size(n_docs);
-    long long most_cols = 0, wide = 0;
-    int longest = 0;
-    for (int i = 0; i < n_docs; ++i) {
-        const PackedQuery q = doc(i);
-        int keys = 0;
-        for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
-        size[i] = {(long long)q.n * G, pk_blocks(keys)};
-        most_cols = std::max(most_cols, size[i].cols);
-        wide += (size[i].cols + pk_cols(PACKED_ROWS) - 1) / pk_cols(PACKED_ROWS) * Hkv;
-        longest = std::max(longest, keys);
+// How the attention of some documents is launched, and its estimated time.
+struct PackedPlan {
+    PackedShape sh;
+    long long range;  // blocks of a key range
+    double steps;
+};
+
+// A plan for the documents (sizes without columns are left out) whose blocks of threads
+// have shape sh.  Key ranges: as many blocks as the device holds at a time and no more,
+// so that none waits for a second round (us a call, with as many blocks and with half as
+// many again: 64 documents of 2000-8000 positions, 32 heads, 80 and 98; 60 documents, 28
+// heads, 48 and 55; 8 documents of 48 rows 57 and 94).  Two steps a wavefront are not
+// worth a split (512 positions, 8.4 us a call in one and 11.5 in two).
+//
+// The estimate counts a wavefront's steps (1.5 us where all wavefronts are busy): the
+// longest block, or a device's share of all of them and a quarter of a last one; two
+// steps for a block's start and end, five for the launches, and the partials' way to
+// memory and back.  It comes within a sixth of most measured calls with many columns.
+hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<PackedSize> &size, PackedShape sh, PackedPlan *out) {
+    const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads, cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
+    const int kw = sh.rows ? 1 : sh.waves / sh.cw;
+    long long units = 0, whole = 1;
+    double work = 0;
+    for (const PackedSize &z : size) {
+        const long long ncg = (z.cols + cols - 1) / cols;
+        units += ncg * Hkv * pk_blocks(z.keys);
+        work += ncg * Hkv * z.mean;
+        if (z.cols > 0) whole = std::max<long long>(whole, pk_blocks(z.keys));
     }
-    // The kernel for many rows once it has a block for every unit (us a call, it and the
-    // other: 4000-token prompt, 32 heads, 297 and 417; two of 1500 tokens 110 and 162; one
-    // of them 106 and 76).
-    PackedShape sh{1, 1, 8, false};
-    if (most_cols <= 16) sh.copies = most_cols <= 4 ? 4 : most_cols <= 8 ? 2 : 1;
-    else if (c->bf16 && wide >= 256) sh = PACKED_ROWS;
-    else sh.cw = most_cols <= 32 ? 2 : 4;
-    const int cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
-    auto count = [&](long long range) {  // blocks with key ranges of `range` blocks of keys, and their number unsplit
+    whole = (whole + sb - 1) / sb * sb;
+    auto count = [&](long long range) {  // blocks of threads with key ranges of `range` blocks of keys
         long long n = 0;
-        for (const Size &z : size) n += (z.cols + cols - 1) / cols * Hkv * std::max<long long>(1, (z.blocks + range - 1) / range);
+        for (const PackedSize &z : size)
+            n += (z.cols + cols - 1) / cols * Hkv * std::max<long long>(1, (pk_blocks(z.keys) + range - 1) / range);
         return n;
     };
-    long long units = 0;
-    for (const Size &z : size) units += (z.cols + cols - 1) / cols * Hkv * z.blocks;
-    // Key ranges: as many blocks as the device holds at a time and no more, so that none
-    // waits for a second round (us a call, with as many blocks and with half as many
-    // again: 64 documents of 2000-8000 positions, 32 heads, 80 and 98; 60 documents, 28
-    // heads, 48 and 55; 8 documents of 48 rows 57 and 94).  Two
-    // steps a wavefront are not worth a split (512 positions, 8.4 us a call in one and
-    // 11.5 in two).  Little work takes blocks of eight wavefronts, whose partials are fewer (one
-    // document of 40001 positions 17.5, blocks of four 18.7); much work for few columns
-    // blocks of four, which come out more even (64 documents 80 and 90).
-    const bool large = most_cols <= 16 && units >= 6ll * 768 * 4 * sb;
-    if (large) sh.waves = 4;
-    const int kw = sh.rows ? 4 : sh.waves / sh.cw;
     PackedAttnArgs probe{};
     probe.hd = c->d.head_dim;
     probe.q_lo = pair ? c->Qb_lo : nullptr;
     int target = 0;
     const hipError_t err = launch_attention_packed(c->bf16, bits, sh, PackedTable{}, probe, nullptr, &target);
     if (err != hipSuccess) return err;
-    const long long whole = (pk_blocks(std::max(longest, 1)) + sb - 1) / sb * sb;
-    long long range = std::max<long long>(kw * sb, (units + target - 1) / target);
-    range = whole <= 2 * kw * sb ? whole : std::min(whole, (range + sb - 1) / sb * sb);
+    const long long least = sh.rows ? 4 : kw * sb;
+    long long range = std::max<long long>(least, (units + target - 1) / target);
+    range = whole <= 2 * least ? whole : std::min(whole, (range + sb - 1) / sb * sb);
     while (range < whole && count(range) > target) range = std::min(whole, range + std::max<long long>(range / 16 / sb * sb, sb));
     const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
     while (range < whole && (whole + range - 1) / range * per_row > slots) range = std::min(whole, range * 2);
-    t.packed_shape = sh;
-    t.packed_range = (int)range * PK_BLOCK;
+    // steps of a block of keys: the kernel for many rows goes through one in 2.2 us (1.6 with
+    // 64 dimensions), 8-bit codes cost a fifth more where they are used as they are, and two
+    // column tiles read the keys twice as often as four
+    const bool wide = pk_width(c->d.head_dim) == 128;
+    const double step = sh.rows ? (wide ? 1.45 : 1.05) : (bits == 8 && wide ? 1.2 : 1.0) * (sh.cw == 2 ? 1.06 : 1.0) / (kw * sb);
+    const double n = (double)count(range), one = range * step + 2;
+    double steps = 5 + (n <= target ? one : (work / PK_BLOCK * step + 2 * n) / target + one / 4);
+    if (range < whole) {
+        double bytes = 0;  // of partials
+        for (const PackedSize &z : size)
+            bytes += (double)z.cols * Hkv * ((pk_blocks(z.keys) + range - 1) / range) * pk_part_row(c->d.head_dim) * 4;
+        steps += 2 * bytes / 6.7e6;  // (4.5 TB/s)
+    }
+    *out = PackedPlan{sh, range, steps};
+    return hipSuccess;
+}
+
+// The plan for a list of documents.
+hipError_t plan_documents(const kvr_ctx *c, int bits, bool pair, const std::vector<PackedSize> &size, PackedPlan *out) {
+    const int Hkv = c->d.n_kv_heads;
+    long long most = 0, units = 0;
+    for (const PackedSize &z : size) {
+        most = std::max(most, z.cols);
+        if (z.cols > 0) units += (long long)Hkv * pk_blocks(z.keys);
+    }
+    *out = PackedPlan{};
+    if (most <= 16) {
+        PackedShape sh{1, 1, 8, false};
+        // Little work takes blocks of eight wavefronts, whose partials are fewer (one
+        // document of 40001 positions 17.5, blocks of four 18.7); much work blocks of four,
+        // which come out more even (64 documents 80 and 90).
+        sh.copies = most <= 4 ? 4 : most <= 8 ? 2 : 1;
+        if (units >= 6ll * 768 * 4 * (sh.copies == 4 ? 2 : 1)) sh.waves = 4;
+        return plan_shape(c, bits, pair, size, sh, out);
+    }
+    // Many columns: two or four tiles of them, or the kernel for many rows (us a call, 32
+    // heads of 8, 4 bits: 20 rows of 32 documents of 6000 positions 236, 304, 362; 48 rows
+    // of 8 156, 154, 114; 200 rows of 4 292, 294, 217; prompts of 1500 tokens 79, 73, 102
+    // and of 4000 437, 408, 290).
+    hipError_t err = hipSuccess;
+    for (const PackedShape s : {PackedShape{4, 1, 8, false}, PackedShape{2, 1, 8, false}, PACKED_ROWS}) {
+        if (s.rows && !c->bf16) continue;
+        PackedPlan p;
+        err = plan_shape(c, bits, pair, size, s, &p);
+        if (err != hipSuccess) return err;
+        if (out->range == 0 || p.steps < out->steps) *out = p;
+    }
+    return err;
+}
+
+// The attention launches of rows over packed caches (t.packed).  pair: the queries are
+// compensated pairs.  Documents with few columns and with many suit different shapes and
+// are launched apart where that is estimated to be faster (us a call: one row of 63
+// documents of 4000 positions and 512 rows of another 105 apart, 166 together; of 4 and
+// 48 rows 32 and 26).
+template <typename DocAt>
+hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_docs, DocAt doc, bool row_table) {
+    const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
+    t.packed.clear();
+    std::vector<PackedSize> size(n_docs), part[2];
+    int few = 0, many = 0;
+    for (int i = 0; i < n_docs; ++i) {
+        const PackedQuery q = doc(i);
+        PackedSize &z = size[i];
+        z.cols = (long long)q.n * G;
+        z.keys = 0;
+        long long sum = 0;
+        for (int r = 0; r < q.n; ++r) {
+            const int sees = q.pos[(size_t)r * q.step] + 1;
+            z.keys = std::max(z.keys, sees);
+            sum += sees;
+        }
+        z.mean = q.n > 0 ? (double)sum / q.n : 0;
+        if (z.cols > 16) ++many;
+        else if (z.cols > 0) ++few;
+    }
+    PackedPlan plan[2];
+    hipError_t err = plan_documents(c, bits, pair, size, &plan[0]);
+    int parts = 1;
+    if (err == hipSuccess && few > 0 && many > 0) {
+        PackedPlan apart[2];
+        for (int p = 0; p < 2 && err == hipSuccess; ++p) {
+            part[p] = size;
+            for (PackedSize &z : part[p])
+                if ((z.cols > 16) != (p == 0)) z.cols = 0;
+            err = plan_documents(c, bits, pair, part[p], &apart[p]);
+        }
+        if (err == hipSuccess && apart[0].steps + apart[1].steps < plan[0].steps) {
+            parts = 2;
+            plan[0] = apart[0];
+            plan[1] = apart[1];
+        }
+    }
+    if (err != hipSuccess) return err;
 
     std::vector<Tables::PackedLaunch> &out = t.packed;
-    TableFill fill(nullptr);
-    int used = 0;  // partial slots of the launch
-    auto open = [&] {
-        out.emplace_back();
-        Tables::PackedLaunch &l = out.back();
-        l.n_docs = l.n_items = l.n_cg = 0;
-        l.splits = 1;
-        fill = TableFill(&l.table);
-        used = 0;
-    };
-    for (int i = 0; i < n_docs; ++i) {
-        PackedQuery q = doc(i);
-        while (q.n > 0) {
-            if (out.empty()) open();
-            int keys = 0;
-            for (int r = 0; r < q.n; ++r) keys = std::max(keys, q.pos[(size_t)r * q.step] + 1);
-            const int ns = std::max(1, (int)((pk_blocks(keys) + range - 1) / range));
-            Tables::PackedLaunch &at = out.back();
-            long long fit = std::max<long long>(PK_MAX_GRID - at.n_items, 0) / ns * cols / G;
-            if (at.n_items == 0) fit = std::max<long long>(fit, 1);  // (a row of many column groups, a small grid)
-            fit = std::min<long long>(fit, q.n);
-            if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);
-            const int before = fill.docs;
-            const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, false, row_table);
-            if (n == 0) {
-                open();
-                continue;
-            }
+    for (int p = 0; p < parts; ++p) {
+        const PackedShape sh = plan[p].sh;
+        const long long range = plan[p].range, cols = pk_cols(sh);
+        const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
+        TableFill fill(nullptr);
+        int used = 0;  // partial slots of the launch
+        auto open = [&] {
+            out.emplace_back();
             Tables::PackedLaunch &l = out.back();
-            uint32_t *e = fill.entry(before);
-            const int ncg = (int)(((long long)n * G + cols - 1) / cols);
-            e[PKE_ITEM0] = (uint32_t)l.n_items;
-            e[PKE_CG0] = (uint32_t)l.n_cg;
-            e[PKE_SPLITS] = (uint32_t)ns;
-            e[PKE_PART0] = (uint32_t)used;
-            e[PKE_KEYS] = (uint32_t)keys;
-            l.n_docs = fill.docs;
-            l.n_items += ncg * ns;
-            l.n_cg += ncg;
-            l.splits = std::max(l.splits, ns);
-            if (ns > 1) used += ncg * ns;
-            q.row0 += n;
-            q.pos += (size_t)n * q.step;
-            q.n -= n;
+            l.sh = sh;
+            l.range = (int)range * PK_BLOCK;
+            l.n_docs = l.n_items = l.n_cg = 0;
+            l.splits = 1;
+            fill = TableFill(&l.table);
+            used = 0;
+        };
+        open();
+        for (int i = 0; i < n_docs; ++i) {
+            if (parts == 2 && (size[i].cols > 16) != (p == 0)) continue;
+            PackedQuery q = doc(i);
+            const int keys = size[i].keys, ns = std::max(1, (int)((pk_blocks(keys) + range - 1) / range));
+            while (q.n > 0) {
+                Tables::PackedLaunch &l = out.back();
+                long long fit = std::max<long long>(PK_MAX_GRID - l.n_items, 0) / ns * cols / G;
+                if (l.n_items == 0) fit = std::max<long long>(fit, 1);  // (a row of many column groups, a small grid)
+                fit = std::min<long long>(fit, q.n);
+                if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);
+                const int before = fill.docs;
+                const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, false, row_table);
+                if (n == 0) {
+                    open();
+                    continue;
+                }
+                uint32_t *e = fill.entry(before);
+                const int ncg = (int)(((long long)n * G + cols - 1) / cols);
+                e[PKE_ITEM0] = (uint32_t)l.n_items;
+                e[PKE_CG0] = (uint32_t)l.n_cg;
+                e[PKE_SPLITS] = (uint32_t)ns;
+                e[PKE_PART0] = (uint32_t)used;
+                e[PKE_KEYS] = (uint32_t)keys;
+                l.n_docs = fill.docs;
+                l.n_items += ncg * ns;
+                l.n_cg += ncg;
+                l.splits = std::max(l.splits, ns);
+                if (ns > 1) used += ncg * ns;
+                q.row0 += n;
+                q.pos += (size_t)n * q.step;
+                q.n -= n;
+            }
         }
     }
     return hipSuccess;
 }
 
 // The kernel arguments of one of plan_packed's launches; `a` describes the rows.
-PackedAttnArgs packed_args(const kvr_ctx *c, const Tables &t, const Tables::PackedLaunch &l, PackedAttnArgs a) {
+PackedAttnArgs packed_args(const kvr_ctx *c, const Tables::PackedLaunch &l, PackedAttnArgs a) {
     a.Hq = c->d.n_heads;
     a.Hkv = c->d.n_kv_heads;
     a.hd = c->d.head_dim;
@@ -738,7 +831,7 @@ PackedAttnArgs packed_args(const kvr_ctx *c, const Tables &t, const Tables::Pack
     a.n_docs = l.n_docs;
     a.n_items = l.n_items;
     a.n_cg = l.n_cg;
-    a.range = t.packed_range;
+    a.range = l.range;
     a.max_splits = l.splits;
     return a;
 }
@@ -915,10 +1008,10 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
         pa.out = c->Ob; pa.out_lo = c->Ob_lo; pa.out_stride = qd; pa.o_perm = op;
         pa.rows = rows; pa.layer = l;
         for (const auto &pl : t.packed) {  // packed caches only
-            KVR_CHECK(launch_attention_packed(bf, bits, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
+            KVR_CHECK(launch_attention_packed(bf, bits, pl.sh, pl.table, packed_args(c, pl, pa), s),
                       "attention_packed", ST_ATTN);
             if (pl.splits > 1)
-                KVR_CHECK(launch_attention_packed_combine(bf, t.packed_shape, pl.table, packed_args(c, t, pl, pa), s),
+                KVR_CHECK(launch_attention_packed_combine(bf, pl.sh, pl.table, packed_args(c, pl, pa), s),
                           "attention_packed_combine", ST_COMBINE);
         }
         if (bits) {
@@ -1329,6 +1422,7 @@ void kvr_destroy(kvr_ctx *c) {
     delete c;
 }
 
+static const char *const TOO_MANY_SLOTS = ": a packed cache has at most 2^30 slots";
 // Bits of a packed cache's codes that a call names.
 static kvr_status check_bits(kvr_ctx *c, const char *who, int32_t bits) {
     return bits == 4 || bits == 8 ? KVR_OK : fail(c, KVR_E_UNSUPPORTED, std::string(who) + ": packed caches hold 4 or 8 bits");
@@ -1343,6 +1437,7 @@ static kvr_status prefill(kvr_ctx *c, const char *name, const int32_t *d_tokens,
     if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, who + ": cache must be 16-byte aligned");
     if (n < 1 || n > n_cap || n_cap > c->d.max_ctx)
         return fail(c, KVR_E_RANGE, who + ": need 1 <= n <= n_cap <= max_ctx");
+    if (bits && n_cap > PK_MAX_SLOTS) return fail(c, KVR_E_RANGE, who + TOO_MANY_SLOTS);
     DeviceGuard g(c->device);
     hipStream_t s = (hipStream_t)stream;
     const int chunk = c->rows_cap;
@@ -1426,6 +1521,7 @@ static kvr_status score(kvr_ctx *c, const char *name, void *d_cache, int32_t bit
     if (m > 1 && !d_logprob) return fail(c, KVR_E_ARG, who + ": NULL log-probability output");
     if (n < 0 || m < 1 || (long long)n + m > n_cap || n_cap > c->d.max_ctx)
         return fail(c, KVR_E_RANGE, who + ": need n >= 0, m >= 1, n + m <= n_cap <= max_ctx");
+    if (bits && n_cap > PK_MAX_SLOTS) return fail(c, KVR_E_RANGE, who + TOO_MANY_SLOTS);
     if (m > c->rows_cap) return fail(c, KVR_E_RANGE, who + ": more appended tokens than one pass holds");
     DeviceGuard g(c->device);
     kvr_status st = score_buffers(c);
@@ -1447,6 +1543,7 @@ static kvr_status generate(kvr_ctx *c, const char *name, void *d_cache, int32_t 
     if (!aligned16(d_cache)) return fail(c, KVR_E_ARG, who + ": cache must be 16-byte aligned");
     if (n < 0 || q < 1 || max_new < 1 || (long long)n + q + max_new - 1 > n_cap || n_cap > c->d.max_ctx)
         return fail(c, KVR_E_RANGE, who + ": need n >= 0, q >= 1, max_new >= 1, n + q + max_new - 1 <= n_cap <= max_ctx");
+    if (bits && n_cap > PK_MAX_SLOTS) return fail(c, KVR_E_RANGE, who + TOO_MANY_SLOTS);
     if (q > c->rows_cap) return fail(c, KVR_E_RANGE, who + ": query longer than one pass holds");
     DeviceGuard g(c->device);
     kvr_status st = score_buffers(c);
@@ -1651,6 +1748,7 @@ static kvr_status repair(kvr_ctx *c, const char *name, const kvr_doc *docs, int3
             return fail(c, KVR_E_ARG, tag + "bad position list");
         if (dc.n < 1 || dc.n > dc.n_cap || dc.n_cap > c->d.max_ctx)
             return fail(c, KVR_E_RANGE, tag + "need 1 <= n <= n_cap <= max_ctx");
+        if (bits && dc.n_cap > PK_MAX_SLOTS) return fail(c, KVR_E_RANGE, tag + (TOO_MANY_SLOTS + 2));
         if (dc.edit_start < 0 || dc.edit_start > dc.edit_end || dc.edit_end > dc.n)
             return fail(c, KVR_E_RANGE, tag + "need 0 <= edit_start <= edit_end <= n");
         for (int j = 0; j < dc.n_positions; ++j) {
@@ -1713,7 +1811,7 @@ kvr_status kvr_repair(kvr_ctx *c, const kvr_doc *docs, int32_t n_docs, void *str
 // ---- packed caches
 
 size_t kvr_packed_bytes(const kvr_dims *d, int32_t n_cap, int32_t bits) {
-    if (!d || n_cap < 0 || (bits != 4 && bits != 8) || check_dims(d) != KVR_OK) return 0;
+    if (!d || n_cap < 0 || n_cap > PK_MAX_SLOTS || (bits != 4 && bits != 8) || check_dims(d) != KVR_OK) return 0;
     return packed_bytes(*d, n_cap, bits);
 }
 
@@ -1746,6 +1844,7 @@ static kvr_status copy_packed(kvr_ctx *c, const char *name, const kvr_pack_doc *
         if (!dc.d_cache || !dc.d_packed) return bad(KVR_E_ARG, "NULL cache");
         if (!aligned16(dc.d_cache) || !aligned16(dc.d_packed)) return bad(KVR_E_ARG, "caches must be 16-byte aligned");
         const int32_t lim = std::min(dc.n_cap, dc.packed_n_cap);
+        if (dc.packed_n_cap > PK_MAX_SLOTS) return bad(KVR_E_RANGE, TOO_MANY_SLOTS + 2);
         if (!dc.h_positions && dc.n_positions > lim) return bad(KVR_E_RANGE, "more positions than a cache has slots");
         if (dc.h_positions) st = check_positions(bad, dc.h_positions, dc.n_positions, 0, lim, true);
         if (st != KVR_OK) return st;
@@ -1825,6 +1924,7 @@ static kvr_status check_packed_rows(kvr_ctx *c, const char *name, int32_t layer,
         if (dc.n_rows == 0) continue;
         if (!dc.d_packed || !aligned16(dc.d_packed)) return bad(KVR_E_ARG, "NULL cache, or not 16-byte aligned");
         if (dc.n_cap < 1 || dc.n_cap > c->d.max_ctx) return bad(KVR_E_RANGE, "need 1 <= n_cap <= max_ctx");
+        if (dc.n_cap > PK_MAX_SLOTS) return bad(KVR_E_RANGE, TOO_MANY_SLOTS + 2);
         st = check_positions(bad, dc.h_positions, dc.n_rows, append ? 0 : -1, dc.n_cap, append);
         if (st != KVR_OK) return st;
         total += dc.n_rows;
@@ -1910,9 +2010,9 @@ static kvr_status attention_packed(kvr_ctx *c, int32_t layer, int32_t bits, cons
     a.out = d_out; a.out_stride = out_stride;
     a.layer = layer;
     for (const auto &l : t.packed) {
-        hipError_t e = launch_attention_packed(c->bf16, bits, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
+        hipError_t e = launch_attention_packed(c->bf16, bits, l.sh, l.table, packed_args(c, l, a), (hipStream_t)stream);
         if (e == hipSuccess && l.splits > 1)
-            e = launch_attention_packed_combine(c->bf16, t.packed_shape, l.table, packed_args(c, t, l, a), (hipStream_t)stream);
+            e = launch_attention_packed_combine(c->bf16, l.sh, l.table, packed_args(c, l, a), (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(c, e, "kvr_attention_packed");
     }
     return KVR_OK;

@@ -11,6 +11,7 @@ namespace kvr {
 
 constexpr int PK_BLOCK = 32;  // positions of a block
 constexpr int PK_GROUP = 64;  // dimensions that share a scale and an offset
+constexpr int PK_MAX_SLOTS = 1 << 30;  // of a cache: positions rounded up to a step's stay within 31 bits
 
 // head_dim as the codes hold it
 __host__ __device__ constexpr int pk_width(int hd) { return hd <= 64 ? 64 : 128; }
@@ -118,7 +119,7 @@ struct PackedAttnArgs {
     int32_t max_splits;     // largest number of key ranges of a document
     // set by the launchers (a block's start is latency: no divisions there that the host
     // can make): Hq / Hkv, log2(e) / sqrt(hd), base-2 logarithms of a block's wavefronts
-    // and of its column tiles, and whether rows can be moved in vectors (pk_vectors)
+    // and of its column tiles, and whether rows can be moved in vectors
     int32_t G;
     float scale;
     int32_t waves_log, cw_log;
@@ -139,8 +140,8 @@ constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
 // device holds at a time (only hd and q_lo of `a` are looked at).
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                    hipStream_t s, int *resident = nullptr);
-// Launch a block of `waves` wavefronts with `lds` bytes, or answer *resident.  `known`:
-// the answers so far, by waves / 4 - 1.
+// The number of blocks of `waves` wavefronts with `lds` bytes that a device holds at a
+// time.  `known`: the answers so far, by waves / 4 - 1.
 template <typename K>
 inline hipError_t pk_resident(K kernel, int waves, size_t lds, std::atomic<int> *known, int *resident) {
     int n = known[waves / 4 - 1].load(std::memory_order_relaxed);

@@ -309,6 +309,35 @@ def test_attention_of_a_whole_prompt(bits, dtype, Hq, Hkv, hd, n):
         check_attention(c, bits, [(0, list(range(n)))], [pack], [dec])
 
 
+@pytest.mark.parametrize("Hq,Hkv,hd,bits", [(256, 16, 128, 4), (256, 16, 128, 8), (240, 16, 96, 4), (256, 16, 64, 4),
+                                            (256, 16, 64, 8), (256, 16, 40, 8), (256, 16, 66, 4)])
+def test_attention_of_a_prompt_with_many_heads(Hq, Hkv, hd, bits):
+    """Enough columns for the kernel that goes through the keys once for many rows; slots behind the rows hold arbitrary
+    bytes."""
+    with Ctx(BF16, Hq, Hkv, hd) as c:
+        pack, dec = fill(c, 420, bits, 5, 500)
+        check_attention(c, bits, [(0, list(range(420)))], [pack], [dec])
+
+
+def test_attention_of_many_rows_over_split_keys():
+    """The same kernel with its keys cut into ranges."""
+    with Ctx(BF16, 256, 4, 128) as c:
+        pack, dec = fill(c, 2990, 4, 5)
+        check_attention(c, 4, [(0, list(range(2890, 2990)))], [pack], [dec])
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,bits", [(BF16, 32, 8, 128, 4), (F32, 8, 8, 64, 8)])
+def test_attention_of_documents_with_one_row_beside_one_with_many(dtype, Hq, Hkv, hd, bits):
+    """A batch that decodes while a prompt runs: the two kinds are launched apart, and every row lands where it belongs."""
+    with Ctx(dtype, Hq, Hkv, hd) as c:
+        ns = [700 + 20 * i for i in range(40)]
+        packs, decs = zip(*[fill(c, n, bits, n) for n in ns])
+        docs = [(i, [n - 1]) for i, n in enumerate(ns)]
+        docs[17] = (17, list(range(ns[17] - 300, ns[17])))
+        docs[30] = (30, [-1])
+        check_attention(c, bits, docs, packs, decs)
+
+
 def test_attention_of_more_documents_and_positions_than_a_table_holds():
     with Ctx(BF16, 4, 2, 64) as c:
         ns = [1 + (37 * i) % 211 for i in range(160)]
@@ -344,11 +373,33 @@ def test_attention_sees_values_that_are_not_finite_only_where_it_should(bits):
         assert torch.isfinite(y[2:4, :, :64]).all() and torch.isfinite(y[4:]).all()
 
 
+@pytest.mark.parametrize("hd,bits", [(64, 8), (128, 4)])
+def test_many_heads_see_values_that_are_not_finite_only_where_they_should(hd, bits):
+    """A NaN value is seen by the rows behind it only, in its group's dimensions only, also when the next blocks are staged
+    over it."""
+    n = 420
+    with Ctx(BF16, 256, 16, hd) as c:
+        pack, _ = fill(c, n, bits, 8, n + 44)
+        p = pack.numpy()
+        bad = np.ones((16, 1, hd), np.float32)
+        bad[:, :, hd - 1] = np.nan  # the last group
+        ref.write(p[0, 1], bad, [137], bits, True)
+        ref.write(p[0, 1], bad, [301], bits, True)
+        ref.write(p[0, 0], bad, [370], bits, False)
+        decs = [[ref.read(p[0, kv], n, hd, bits, kv == 1) for kv in range(2)]]
+        rows = list(range(n))
+        body = check_attention(c, bits, [(0, rows)], [torch.tensor(p)], decs)
+        y = body.view(n, 256, hd).float()
+        for r in rows:
+            assert torch.isnan(y[r, :, hd - 64:]).all() == (r >= 137)
+            if hd > 64:  # the other group's dimensions
+                assert torch.isfinite(y[r, :, :hd - 64]).all() == (r < 370)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_many_rows_see_values_that_are_not_finite_only_where_they_should(bits, hd):
-    """The same for the kernel that goes through the keys once for many rows: a NaN value is seen by the rows behind it
-    only, in its group's dimensions only, also when the next blocks are staged over it."""
+    """The same for rows of few heads."""
     with Ctx(BF16, 8, 2, hd) as c:
         pack, _ = fill(c, 300, bits, 8, 320)
         p = pack.numpy()
@@ -506,6 +557,7 @@ def test_refusals():
             refused(R, fn, c.ctx, d(C, 128, P, 64, 65), 4, s)
             refused(R, fn, c.ctx, d(C, 128, P, 64, [64]), 4, s)
             refused(R, fn, c.ctx, d(C, 128, P, 128, [-1]), 4, s)
+            refused(R, fn, c.ctx, d(C, 128, P, 2 ** 30 + 1, [1]), 4, s)
             refused(A, fn, c.ctx, d(C, 128, P, 128, [3, 3]), 4, s)
             refused(A, fn, c.ctx, d(C, 128, P, 128, [3, 2]), 4, s)
             two = kvr.make_pack_docs([(C, 64, P, 64, 10), (C, 64, P, 64, 10)])

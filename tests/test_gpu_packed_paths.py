@@ -125,6 +125,21 @@ def test_prefill_packed(shape, dtype, bits):
         assert e <= TOL[dtype]
 
 
+def test_prefill_packed_with_many_heads():
+    """Enough columns for the attention kernel for many rows, with the decoder's compensated queries."""
+    n, shape = 300, synth.ModelShape("many-heads", 1, 256, 256, 16, 128, 320, 512, 1e-5, 1e5)
+    with Packed(shape, kvr.KVR_BF16, n + 9, n, 4) as p:
+        toks = synth.make_tokens(n, shape.vocab)
+        before = p.bytes().copy()
+        hidden = torch.zeros((n, shape.d_model), device="cuda")
+        dev = toks.cuda()
+        kvr.kvr_prefill_packed(p.ctx, dev.data_ptr(), n, n + 9, p.cache.data_ptr(), 4, hidden.data_ptr(), stream())
+        y = check_pass(p, before, p.bytes(), toks.numpy(), range(n), n + 9, "prefill")
+        e = relmax(hidden.cpu().numpy(), y)
+        say(f"prefill {shape.name}: hidden {e:.2e}")
+        assert e <= TOL[kvr.KVR_BF16]
+
+
 @pytest.mark.parametrize("shape,dtype,bits", CASES)
 @pytest.mark.parametrize("span,K", [(8, 24), (3, 0), (16, 130)])
 def test_repair_packed(shape, dtype, bits, span, K):

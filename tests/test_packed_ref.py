@@ -88,6 +88,9 @@ def test_packed_bytes(hd, bits, n_cap):
 def test_packed_bytes_refusals():
     assert kvr.kvr_packed_bytes(_dims(), 32, 5) == 0
     assert kvr.kvr_packed_bytes(_dims(), -1, 4) == 0
+    assert kvr.kvr_packed_bytes(_dims(), 2 ** 30, 4) > 2 ** 30
+    assert kvr.kvr_packed_bytes(_dims(), 2 ** 30 + 1, 4) == 0
+    assert kvr.kvr_packed_bytes(_dims(), 2 ** 31 - 1, 4) == 0
     assert kvr.kvr_packed_bytes(_dims(head_dim=256), 32, 4) == 0
     assert kvr.load().kvr_packed_bytes(None, 32, 4) == 0
 
