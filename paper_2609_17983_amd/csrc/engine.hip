@@ -638,9 +638,10 @@ struct PackedPlan {
 // worth a split (512 positions, 8.4 us a call in one and 11.5 in two).
 //
 // The estimate counts a wavefront's steps (1.5 us where all wavefronts are busy): the
-// longest block, or a device's share of all of them and a quarter of a last one; two
-// steps for a block's start and end, five for the launches, and the partials' way to
-// memory and back.  It comes within a sixth of most measured calls with many columns.
+// longest block; if there are more blocks than a device holds, rounds of them if they
+// are alike, otherwise a device's share of all and a quarter of a last one; two steps
+// for a block's start and end, five for the launches, and the partials' way to memory
+// and back.  It comes within a sixth of most measured calls with many columns.
 hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<PackedSize> &size, PackedShape sh, PackedPlan *out) {
     const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads, cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
     const int kw = sh.rows ? 1 : sh.waves / sh.cw;
@@ -677,15 +678,27 @@ hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<P
     // column tiles read the keys twice as often as four
     const bool wide = pk_width(c->d.head_dim) == 128;
     const double step = sh.rows ? (wide ? 1.45 : 1.05) : (bits == 8 && wide ? 1.2 : 1.0) * (sh.cw == 2 ? 1.06 : 1.0) / (kw * sb);
-    const double n = (double)count(range), one = range * step + 2;
-    double steps = 5 + (n <= target ? one : (work / PK_BLOCK * step + 2 * n) / target + one / 4);
-    if (range < whole) {
-        double bytes = 0;  // of partials
-        for (const PackedSize &z : size)
-            bytes += (double)z.cols * Hkv * ((pk_blocks(z.keys) + range - 1) / range) * pk_part_row(c->d.head_dim) * 4;
-        steps += 2 * bytes / 6.7e6;  // (4.5 TB/s)
-    }
-    *out = PackedPlan{sh, range, steps};
+    const bool even = work >= 0.9 * PK_BLOCK * units;  // (a prompt's blocks are not)
+    auto estimate = [&](long long range) {
+        const double n = (double)count(range), one = range * step + 2;
+        double steps = 5 + (n <= target ? one : even ? std::ceil(n / target) * one : (work / PK_BLOCK * step + 2 * n) / target + one / 4);
+        if (range < whole) {
+            double bytes = 0;  // of partials
+            for (const PackedSize &z : size)
+                bytes += (double)z.cols * Hkv * ((pk_blocks(z.keys) + range - 1) / range) * pk_part_row(c->d.head_dim) * 4;
+            steps += 2 * bytes / 6.7e6;  // (4.5 TB/s)
+        }
+        return steps;
+    };
+    *out = PackedPlan{sh, range, estimate(range)};
+    // More blocks than that can still be faster: a last round that is part empty is shorter.
+    if (sh.cw > 1)
+        for (int k = 2; k <= 4; ++k) {
+            const long long r = (whole + k - 1) / k;
+            if (r >= range || r < 4 * least || k * per_row > slots) break;
+            const double steps = estimate(r);
+            if (steps < 0.95 * out->steps) *out = PackedPlan{sh, r, steps};
+        }
     return hipSuccess;
 }
 
