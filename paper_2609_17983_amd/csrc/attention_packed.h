@@ -322,9 +322,9 @@ __device__ __forceinline__ void pk_query(const PackedAttnArgs &a, int64_t row, i
 }
 
 // T: the model's type.  QP: bf16 pieces of a query; CL: copies of the columns in a
-// tile.
-template <typename T, int HP, int BITS, int QP, int CL>
-__global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedAttnArgs a, PackedTable t) {
+// tile; N: words of the table.
+template <typename T, int HP, int BITS, int QP, int CL, int N>
+__global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(PackedAttnArgs a, PackedWords<N> t) {
     constexpr int KS = HP / 32, GS = HP / PK_GROUP, DT = HP / 16;
     constexpr int PP = sizeof(T) == 4 ? 3 : 2;  // bf16 pieces of a probability times a scale
     constexpr bool CENTRED = sizeof(T) == 4;
@@ -620,8 +620,11 @@ template <typename T, int HP, int BITS, int QP, int CL>
 hipError_t pk_launch(const PackedTable &t, const PackedAttnArgs &a, PackedShape sh, hipStream_t s, int *resident) {
     const uint32_t lds = (uint32_t)sh.waves * (HP / 16 * 256 + 128) * 4;  // the wavefronts' states
     static std::atomic<int> known[2];
-    if (resident) return pk_resident(attention_packed_kernel<T, HP, BITS, QP, CL>, sh.waves, lds, known, resident);
-    kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, a, t);
+    if (resident) return pk_resident(attention_packed_kernel<T, HP, BITS, QP, CL, PK_WORDS>, sh.waves, lds, known, resident);
+    pk_with_words(t, a.n_docs, [&](const auto &words) {
+        constexpr int N = sizeof(words) / 4;
+        kvr_launch((attention_packed_kernel<T, HP, BITS, QP, CL, N>), dim3(a.Hkv, a.n_items), dim3(64 * sh.waves), lds, s, a, words);
+    });
     return hipGetLastError();
 }
 

@@ -11,8 +11,8 @@ namespace {
 // Joins the partials of a column's key ranges.  HP / 4 lanes read a partial; a column's
 // WC wavefronts take WC * 256 / HP ranges at a time, UN of them in flight, each group
 // keeps a running maximum, and the groups are joined through LDS.
-template <typename T, int HP, int WC>
-__global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedAttnArgs a, PackedTable t, int cols_log) {
+template <typename T, int HP, int WC, int N>
+__global__ __launch_bounds__(256) void attention_packed_combine_kernel(PackedAttnArgs a, PackedWords<N> t, int cols_log) {
     constexpr int L = HP / 4, GR = 64 / L, UN = 4;
     __shared__ float red[4][64][6];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kvh = blockIdx.y;
@@ -110,19 +110,22 @@ hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const Pack
     const PackedAttnArgs a = pk_complete(bf16, sh, args);
     const int wc = a.max_splits > 8 ? 4 : 1;
     const dim3 grid((unsigned)(((size_t)a.n_cg * cols * wc + 3) / 4), a.Hkv);
-#define KVR_COMBINE(T, HP)                                                                                                    \
-    do {                                                                                                                      \
-        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4>), grid, dim3(256), 0, s, a, t, cols_log);       \
-        else kvr_launch((attention_packed_combine_kernel<T, HP, 1>), grid, dim3(256), 0, s, a, t, cols_log);               \
+    pk_with_words(t, a.n_docs, [&](const auto &words) {
+        constexpr int N = sizeof(words) / 4;
+#define KVR_COMBINE(T, HP)                                                                                                      \
+    do {                                                                                                                        \
+        if (wc == 4) kvr_launch((attention_packed_combine_kernel<T, HP, 4, N>), grid, dim3(256), 0, s, a, words, cols_log); \
+        else kvr_launch((attention_packed_combine_kernel<T, HP, 1, N>), grid, dim3(256), 0, s, a, words, cols_log);         \
     } while (0)
-    if (pk_width(a.hd) == 64) {
-        if (bf16) KVR_COMBINE(bf16_t, 64);
-        else KVR_COMBINE(float, 64);
-    } else {
-        if (bf16) KVR_COMBINE(bf16_t, 128);
-        else KVR_COMBINE(float, 128);
-    }
+        if (pk_width(a.hd) == 64) {
+            if (bf16) KVR_COMBINE(bf16_t, 64);
+            else KVR_COMBINE(float, 64);
+        } else {
+            if (bf16) KVR_COMBINE(bf16_t, 128);
+            else KVR_COMBINE(float, 128);
+        }
 #undef KVR_COMBINE
+    });
     return hipGetLastError();
 }
 

@@ -518,8 +518,15 @@ size_t packed_bytes(const kvr_dims &d, int32_t n_cap, int bits) {
 struct TableFill {
     PackedTable *t;
     int docs = 0, tail = PK_WORDS;
-    explicit TableFill(PackedTable *table) : t(table) {}
-    uint32_t *entry(int i) { return t->w + i * PK_ENTRY; }
+    explicit TableFill(PackedTable *table) : t(table) {
+        if (t) t->tail = tail;
+    }
+    uint32_t *entry(int i) { return t->words.w + i * PK_ENTRY; }
+    uint32_t take(int words) {  // of the table's end; what REF says of them
+        tail -= words;
+        t->tail = tail;
+        return (uint32_t)(PK_WORDS - tail);
+    }
     // An entry for the first rows of a list of n positions (`step` words apart):
     // returns how many, 0 when the table is full.  A run of consecutive positions
     // needs no list; one of an entry's length or more gets an entry of its own if
@@ -548,9 +555,8 @@ struct TableFill {
                 }
                 k = std::min(std::min(last, n), room);
                 if (k < 1) return 0;
-                tail -= k;
-                ref = (uint32_t)tail;
-                for (int i = 0; i < k; ++i) t->w[tail + i] = (uint32_t)pos[(size_t)i * step];
+                ref = take(k);
+                for (int i = 0; i < k; ++i) t->words.w[tail + i] = (uint32_t)pos[(size_t)i * step];
             }
         }
         uint32_t *e = entry(docs++);
@@ -594,12 +600,11 @@ struct TableFill {
                 uint32_t mask = 0;
                 for (; i < n && pos[i] / PK_BLOCK == b; ++i) mask |= 1u << pos[i] % PK_BLOCK;
                 ++m;
-                t->w[tail - 2 * m] = (uint32_t)b;
-                t->w[tail - 2 * m + 1] = mask;
+                t->words.w[tail - 2 * m] = (uint32_t)b;
+                t->words.w[tail - 2 * m + 1] = mask;
             }
             if (m == 0) return nullptr;
-            tail -= 2 * m;
-            e[PKE_REF] = (uint32_t)tail;
+            e[PKE_REF] = take(2 * m);
             *taken = i;
             *units = m;
         }
@@ -664,7 +669,8 @@ hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<P
     probe.hd = c->d.head_dim;
     probe.q_lo = pair ? c->Qb_lo : nullptr;
     int target = 0;
-    const hipError_t err = launch_attention_packed(c->bf16, bits, sh, PackedTable{}, probe, nullptr, &target);
+    static const PackedTable none{};
+    const hipError_t err = launch_attention_packed(c->bf16, bits, sh, none, probe, nullptr, &target);
     if (err != hipSuccess) return err;
     const long long least = sh.rows ? 4 : kw * sb;
     long long range = std::max<long long>(least, (units + target - 1) / target);

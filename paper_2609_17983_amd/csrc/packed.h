@@ -3,6 +3,7 @@
 // over them.
 #pragma once
 
+#include <algorithm>
 #include <atomic>
 
 #include "common.h"
@@ -53,16 +54,23 @@ __host__ __device__ __forceinline__ int pk_value_byte(int hp, int bits, int r, i
 // The documents and positions of one launch, in the kernel's argument (HIP's
 // limit is 4 KB), so that a call stages nothing in memory and a captured one
 // keeps its own.  Entries of PK_ENTRY words stand at the front, positions at the
-// back.
-constexpr int PK_WORDS = 896, PK_ENTRY = 12;
+// back (from word `tail` on).  What fits PK_FEW_WORDS is passed in as many: 3.6 KB
+// of arguments take the host 0.9 us longer a launch, and a call on an idle device
+// ends 5 us later (one document of 509 positions: 28 us, 22).
+constexpr int PK_WORDS = 896, PK_FEW_WORDS = 64, PK_ENTRY = 12;
 constexpr int PK_MAX_DOCS = PK_WORDS / PK_ENTRY;
+template <int N>
+struct PackedWords {
+    alignas(8) uint32_t w[N];
+};
 struct PackedTable {
-    alignas(8) uint32_t w[PK_WORDS];
+    PackedWords<PK_WORDS> words;
+    int tail = PK_WORDS;
 };
 // Words of an entry.  Rows r of an entry are rows ROW0 + r of the launch's row
-// arrays; their positions are POS + r (POS >= 0 or -1) when REF is
-// PK_RUN, word REF + r of the table, or, when REF is PK_ROWS, those of the pass's
-// row table.
+// arrays; their positions are POS + r (POS >= 0 or -1) when REF is PK_RUN, those of
+// the pass's row table when it is PK_ROWS, otherwise the words REF - r before the
+// table's end.
 enum {
     PKE_PACKED = 0,  // packed cache (two words)
     PKE_BLOCKS = 2,  // its blocks per plane
@@ -78,9 +86,9 @@ enum {
     PKE_PART0 = 10,
     PKE_KEYS = 11,
     // copies: the units (blocks with listed positions) of the entry, by the first one's
-    // index in the launch; POS and RUN are a run of positions, otherwise word REF + 2 i
-    // is unit i's block and the next one the mask of its positions; the cache (two
-    // words) and its rows per plane
+    // index in the launch; POS and RUN are a run of positions, otherwise the words REF - 2 i
+    // before the table's end are unit i's block and the mask of its positions; the cache
+    // (two words) and its rows per plane
     PKC_UNIT0 = 3,
     PKC_CACHE = 7,
     PKC_NCAP = 9,
@@ -163,10 +171,11 @@ hipError_t launch_attention_packed_combine(bool bf16, PackedShape sh, const Pack
 #ifdef __HIPCC__
 // Entry of a launch that holds index `x`: the last one whose word `word` is not
 // above it.  Every lane looks at one entry, so the search is one load deep.
-__device__ __forceinline__ int pk_find(const PackedTable &t, int n_docs, int word, int x) {
+template <int N>
+__device__ __forceinline__ int pk_find(const PackedWords<N> &t, int n_docs, int word, int x) {
     if (n_docs == 1) return 0;
     const int lane = threadIdx.x & 63;
-    constexpr int B = (PK_MAX_DOCS + 63) / 64;
+    constexpr int B = (N / PK_ENTRY + 63) / 64;
     int v[B], n = 0;
 #pragma unroll
     for (int b = 0; b < B; ++b) v[b] = (int)t.w[min(b * 64 + lane, n_docs - 1) * PK_ENTRY + word];
@@ -184,22 +193,38 @@ struct PackedEntry {
 static_assert(sizeof(PackedEntry) == PK_ENTRY * 4, "entry words");
 // The entry that holds index x.  The first one is loaded with the arguments, so that
 // the usual launch of one document has no second round trip.
-__device__ __forceinline__ PackedEntry pk_entry(const PackedTable &t, int n_docs, int word, int x) {
+template <int N>
+__device__ __forceinline__ PackedEntry pk_entry(const PackedWords<N> &t, int n_docs, int word, int x) {
     PackedEntry e = *reinterpret_cast<const PackedEntry *>(t.w);
     if (n_docs > 1) e = *reinterpret_cast<const PackedEntry *>(t.w + pk_find(t, n_docs, word, x) * PK_ENTRY);
     return e;
 }
-__device__ __forceinline__ int pk_position(const PackedTable &t, const PackedEntry &e, int r, const RowInfo *rows) {
+template <int N>
+__device__ __forceinline__ int pk_position(const PackedWords<N> &t, const PackedEntry &e, int r, const RowInfo *rows) {
     if (e.ref == PK_RUN) return e.pos + r;
     if (e.ref == PK_ROWS) return rows[e.row0 + r].pos;
-    return (int)t.w[e.ref + r];
+    return (int)t.w[N - e.ref + r];
 }
 __device__ __forceinline__ char *pk_pointer(const uint32_t *e) {
     return (char *)(((uint64_t)e[1] << 32) | e[0]);
 }
 // Position of row r of entry e of an append.
-__device__ __forceinline__ int pk_position(const PackedTable &t, const uint32_t *e, int r) {
-    return e[PKE_REF] == PK_RUN ? (int)e[PKE_POS] + r : (int)t.w[e[PKE_REF] + r];
+template <int N>
+__device__ __forceinline__ int pk_position(const PackedWords<N> &t, const uint32_t *e, int r) {
+    return e[PKE_REF] == PK_RUN ? (int)e[PKE_POS] + r : (int)t.w[N - e[PKE_REF] + r];
+}
+// launch(words) with the words that a launch's table needs.
+template <typename Launch>
+inline void pk_with_words(const PackedTable &t, int n_docs, Launch launch) {
+    const int front = n_docs * PK_ENTRY, back = PK_WORDS - t.tail;
+    if (front + back > PK_FEW_WORDS) {
+        launch(t.words);
+        return;
+    }
+    PackedWords<PK_FEW_WORDS> few;
+    std::copy(t.words.w, t.words.w + front, few.w);
+    std::copy(t.words.w + t.tail, t.words.w + PK_WORDS, few.w + PK_FEW_WORDS - back);
+    launch(few);
 }
 #endif
 

@@ -92,9 +92,10 @@ __device__ __forceinline__ void write_row(const float x[2], int hd, bool value, 
     }
 }
 
-// One wavefront per (row, plane): fresh rows of one layer.
-template <typename T, int HP, int BITS>
-__global__ __launch_bounds__(256) void packed_append_kernel(PackedTable t, int n_docs, const T *k, const T *v,
+// One wavefront per (row, plane): fresh rows of one layer.  Bound by its start and one
+// round of loads: 64 rows of 8 heads 4.2 us, 528 rows of 4 heads 5.4 us.
+template <typename T, int HP, int BITS, int N>
+__global__ __launch_bounds__(256) void packed_append_kernel(PackedWords<N> t, int n_docs, const T *k, const T *v,
                                                             int64_t stride, int layer, int Hkv, int hd) {
     const int lane = threadIdx.x & 63, plane = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t *first = t.w;
@@ -118,14 +119,18 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedTable t, int n
 // the two halves of a value byte are in one lane and a key word is one lane's.  The
 // packed block is put together (or taken apart) in LDS and moves to and from memory
 // in one contiguous piece; where only some positions are listed, their words and
-// bytes move one by one and the others are not touched.
+// bytes move one by one and the others are not touched.  Bound by memory: 32 layers of 8
+// heads, 5000 positions, 4 bits (839 MB) 192 us packed and 178 us read back, 4.4 and
+// 4.7 TB/s (a large copy 4.9).  By one row a wavefront, straight to memory, the two took
+// 1960 us.
 struct PackedUnit {
     char *block;     // the packed block
     size_t row;      // index of the block's first position among the cache's rows
     const uint32_t *e;
     uint32_t mask;
 };
-__device__ __forceinline__ PackedUnit pk_unit(const PackedTable &t, int n_docs, int unit, int plane, int block_bytes) {
+template <int N>
+__device__ __forceinline__ PackedUnit pk_unit(const PackedWords<N> &t, int n_docs, int unit, int plane, int block_bytes) {
     PackedUnit u;
     u.e = t.w + pk_find(t, n_docs, PKC_UNIT0, unit) * PK_ENTRY;
     const int i = unit - (int)u.e[PKC_UNIT0];
@@ -136,8 +141,8 @@ __device__ __forceinline__ PackedUnit pk_unit(const PackedTable &t, int n_docs, 
         const int lo = max(p0 - b * PK_BLOCK, 0), hi = min(p1 - b * PK_BLOCK, PK_BLOCK);
         u.mask = (0xffffffffu >> (32 - (hi - lo))) << lo;
     } else {
-        b = t.w[u.e[PKE_REF] + 2 * i];
-        u.mask = t.w[u.e[PKE_REF] + 2 * i + 1];
+        b = t.w[N - u.e[PKE_REF] + 2 * i];
+        u.mask = t.w[N - u.e[PKE_REF] + 2 * i + 1];
     }
     u.block = pk_pointer(u.e) + ((size_t)plane * u.e[PKE_BLOCKS] + b) * block_bytes;
     u.row = (size_t)plane * u.e[PKC_NCAP] + (size_t)b * PK_BLOCK;
@@ -188,7 +193,7 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
         for (int q = 0; q < 4; ++q)
             v[q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * q], x[2 * q + 1]}, bf16x2));
         // a line leaves in one instruction and is not read again here: past the caches
-        // (28 layers of 4-bit codes, 5000 positions: 84 -> 61 us, 6.0 TB/s)
+        // (28 layers of 4-bit codes, 4 heads, 5000 positions: 84 -> 56 us, 6.5 TB/s)
         __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p + d));
     } else if (!vec) {
 #pragma unroll
@@ -197,8 +202,8 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
     }
 }
 
-template <typename T, int HP, int BITS, bool UNPACK>
-__global__ __launch_bounds__(256) void packed_copy_kernel(PackedTable t, int n_docs, int n_units, int hd, int Hkv, int plane0) {
+template <typename T, int HP, int BITS, bool UNPACK, int N>
+__global__ __launch_bounds__(256) void packed_copy_kernel(PackedWords<N> t, int n_docs, int n_units, int hd, int Hkv, int plane0) {
     constexpr int GS = HP / PK_GROUP, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
     constexpr int TPR = HP / 16, TPU = PK_BLOCK * TPR, NU = 256 / TPU;  // lanes of a row, of a unit; units
     __shared__ __attribute__((aligned(16))) char lds[NU][BB];
@@ -403,15 +408,18 @@ hipError_t launch_packed_append(bool bf16, int bits, const PackedTable &t, int n
     if (n_rows <= 0) return hipSuccess;
     if (n_docs < 1 || n_docs > PK_MAX_DOCS || hd > 128 || (bits != 4 && bits != 8)) return hipErrorInvalidValue;
     const dim3 grid(n_rows, (2 * Hkv + 3) / 4);
-#define KVR_CALL(HP, BITS)                                                                                             \
-    if (bf16)                                                                                                          \
-        kvr_launch((packed_append_kernel<bf16_t, HP, BITS>), grid, dim3(256), 0, s, t, n_docs, (const bf16_t *)k,      \
-                   (const bf16_t *)v, stride, layer, Hkv, hd);                                                         \
-    else                                                                                                               \
-        kvr_launch((packed_append_kernel<float, HP, BITS>), grid, dim3(256), 0, s, t, n_docs, (const float *)k,        \
+    pk_with_words(t, n_docs, [&](const auto &words) {
+        constexpr int N = sizeof(words) / 4;
+#define KVR_CALL(HP, BITS)                                                                                              \
+    if (bf16)                                                                                                           \
+        kvr_launch((packed_append_kernel<bf16_t, HP, BITS, N>), grid, dim3(256), 0, s, words, n_docs, (const bf16_t *)k, \
+                   (const bf16_t *)v, stride, layer, Hkv, hd);                                                          \
+    else                                                                                                                \
+        kvr_launch((packed_append_kernel<float, HP, BITS, N>), grid, dim3(256), 0, s, words, n_docs, (const float *)k,  \
                    (const float *)v, stride, layer, Hkv, hd)
-    KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
+        KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
 #undef KVR_CALL
+    });
     return hipGetLastError();
 }
 
@@ -422,16 +430,19 @@ hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTabl
     const int units = pk_width(hd) == 64 ? 2 : 1;
     for (int p0 = 0; p0 < planes; p0 += 32768) {
         const dim3 grid((n_units + units - 1) / units, std::min(planes - p0, 32768));
+        pk_with_words(t, n_docs, [&](const auto &words) {
+            constexpr int N = sizeof(words) / 4;
 #define KVR_COPY(T, HP, BITS, UN) \
-    kvr_launch((packed_copy_kernel<T, HP, BITS, UN>), grid, dim3(256), 0, s, t, n_docs, n_units, hd, Hkv, p0)
+    kvr_launch((packed_copy_kernel<T, HP, BITS, UN, N>), grid, dim3(256), 0, s, words, n_docs, n_units, hd, Hkv, p0)
 #define KVR_CALL(HP, BITS)                                   \
     if (bf16 && unpack) KVR_COPY(bf16_t, HP, BITS, true);    \
     else if (bf16) KVR_COPY(bf16_t, HP, BITS, false);        \
     else if (unpack) KVR_COPY(float, HP, BITS, true);        \
     else KVR_COPY(float, HP, BITS, false)
-        KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
+            KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
 #undef KVR_CALL
 #undef KVR_COPY
+        });
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
