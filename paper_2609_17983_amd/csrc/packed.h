@@ -206,7 +206,8 @@ __device__ __forceinline__ int pk_position(const PackedWords<N> &t, const Packed
     return (int)t.w[N - e.ref + r];
 }
 __device__ __forceinline__ char *pk_pointer(const uint32_t *e) {
-    return (char *)(((uint64_t)e[1] << 32) | e[0]);
+    // (into device memory: its accesses need not be those of any address)
+    return (char *)(__attribute__((address_space(1))) char *)(((uint64_t)e[1] << 32) | e[0]);
 }
 // Position of row r of entry e of an append.
 template <int N>

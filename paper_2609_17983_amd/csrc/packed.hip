@@ -120,8 +120,9 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedWords<N> t, in
 // packed block is put together (or taken apart) in LDS and moves to and from memory
 // in one contiguous piece; where only some positions are listed, their words and
 // bytes move one by one and the others are not touched.  Bound by memory: 32 layers of 8
-// heads, 5000 positions, 4 bits (839 MB) 192 us packed and 178 us read back, 4.4 and
-// 4.7 TB/s (a large copy 4.9).  By one row a wavefront, straight to memory, the two took
+// heads, 5000 positions, 4 bits (839 MB) 159 us packed and 139 us read back, 5.3 and
+// 6.0 TB/s (a large copy 4.9: the packed cache is partly in the last-level cache); with
+// loads that wait for each other and masks for partial rows it was 192 and 178.  By one row a wavefront, straight to memory, the two took
 // 1960 us.
 struct PackedUnit {
     char *block;     // the packed block
@@ -149,30 +150,36 @@ __device__ __forceinline__ PackedUnit pk_unit(const PackedWords<N> &t, int n_doc
     return u;
 }
 
-// Eight values from dimension d on, zeros behind hd; vec: hd is a multiple of 8 (rows
-// are then 16-byte aligned).
-__device__ __forceinline__ void pk_load8(const float *p, int d, int hd, bool vec, float *x) {
+// The eight values from dimension d on and the eight 16 further, zeros behind hd; vec: hd
+// is a multiple of 8 (rows are then 16-byte aligned).
+__device__ __forceinline__ void pk_load16(const float *p, int d, int hd, bool vec, float x[2][8]) {
     if (vec) {
-        const bool in = d < hd;
+        f32x4 v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const f32x4 *>(p + min(d + 16 * (q >> 1), hd - 8) + 4 * (q & 1));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[q >> 1][4 * (q & 1) + i] = d + 16 * (q >> 1) < hd ? v[q][i] : 0.f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] = d + i + (i & 8) < hd ? p[d + i + (i & 8)] : 0.f;
+    }
+}
+__device__ __forceinline__ void pk_load16(const bf16_t *p, int d, int hd, bool vec, float x[2][8]) {
+    if (vec) {
+        u32x4 v[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) v[q] = *reinterpret_cast<const u32x4 *>(p + min(d + 16 * q, hd - 8));
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const f32x4 v = in ? *reinterpret_cast<const f32x4 *>(p + d + 4 * q) : f32x4{0.f, 0.f, 0.f, 0.f};
+            const u32x4 u = d + 16 * q < hd ? v[q] : u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
+            for (int i = 0; i < 8; ++i) x[q][i] = __uint_as_float(i & 1 ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = d + i < hd ? p[d + i] : 0.f;
-    }
-}
-__device__ __forceinline__ void pk_load8(const bf16_t *p, int d, int hd, bool vec, float *x) {
-    if (vec) {
-        const u32x4 v = d < hd ? *reinterpret_cast<const u32x4 *>(p + d) : u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = d + i < hd ? bf16_to_f32(p[d + i]) : 0.f;
+        for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] = d + i + (i & 8) < hd ? bf16_to_f32(p[d + i + (i & 8)]) : 0.f;
     }
 }
 __device__ __forceinline__ void pk_store8(float *p, int d, int hd, bool vec, const float *x) {
@@ -193,7 +200,7 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
         for (int q = 0; q < 4; ++q)
             v[q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * q], x[2 * q + 1]}, bf16x2));
         // a line leaves in one instruction and is not read again here: past the caches
-        // (28 layers of 4-bit codes, 4 heads, 5000 positions: 84 -> 56 us, 6.5 TB/s)
+        // (28 layers of 4-bit codes, 4 heads, 5000 positions: 84 -> 56 us a call, 52 now, 7.0 TB/s)
         __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p + d));
     } else if (!vec) {
 #pragma unroll
@@ -202,8 +209,10 @@ __device__ __forceinline__ void pk_store8(bf16_t *p, int d, int hd, bool vec, co
     }
 }
 
-template <typename T, int HP, int BITS, bool UNPACK, int N>
-__global__ __launch_bounds__(256) void packed_copy_kernel(PackedWords<N> t, int n_docs, int n_units, int hd, int Hkv, int plane0) {
+// FULL: hd is HP.
+template <typename T, int HP, int BITS, bool UNPACK, bool FULL, int N>
+__global__ __launch_bounds__(256) void packed_copy_kernel(PackedWords<N> t, int n_docs, int n_units, int head_dim, int Hkv, int plane0) {
+    const int hd = FULL ? HP : head_dim;
     constexpr int GS = HP / PK_GROUP, BB = pk_block_bytes(HP, BITS), CB = pk_code_bytes(HP, BITS);
     constexpr int TPR = HP / 16, TPU = PK_BLOCK * TPR, NU = 256 / TPU;  // lanes of a row, of a unit; units
     __shared__ __attribute__((aligned(16))) char lds[NU][BB];
@@ -212,7 +221,7 @@ __global__ __launch_bounds__(256) void packed_copy_kernel(PackedWords<N> t, int 
     const int unit = min((int)blockIdx.x * NU + sub, n_units - 1);  // a last odd one is done twice, alike
     const int plane = plane0 + blockIdx.y;
     const PackedUnit u = pk_unit(t, n_docs, unit, plane, BB);
-    const bool value = plane / Hkv & 1, vec = hd % 8 == 0, mine = u.mask >> r & 1;
+    const bool value = plane / Hkv & 1, vec = FULL || hd % 8 == 0, mine = u.mask >> r & 1;
     T *row = (T *)pk_pointer(u.e + PKC_CACHE) + (u.row + r) * hd;
     char *b = lds[sub];
     uint32_t *words = reinterpret_cast<uint32_t *>(b);
@@ -231,23 +240,29 @@ __global__ __launch_bounds__(256) void packed_copy_kernel(PackedWords<N> t, int 
             const uint32_t w = *reinterpret_cast<const uint32_t *>(b + CB + (r * GS + d1 / PK_GROUP) * 4);
             const float off = __uint_as_float(w & 0xffff0000u), s = __uint_as_float(w << 16);
             float x[8];
+            auto element = [&](int i, uint32_t c) {
+                x[i] = fmaf(s, (float)(c & ((1u << BITS) - 1)), off);  // (the product is exact: 8 significant bits each)
+            };
+            int bit;
+            if (value) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                int bit;
-                const int at = value ? pk_value_byte(HP, BITS, r, d1 + i, &bit) : pk_key_byte(HP, BITS, r, d1 + i, &bit);
-                const uint32_t c = (value ? (uint32_t)(uint8_t)b[at] >> bit : words[at >> 2] >> (8 * (at & 3) + bit)) & ((1u << BITS) - 1);
-                x[i] = fmaf(s, (float)c, off);  // (the product is exact: 8 significant bits each)
+                for (int i = 0; i < 8; ++i) {
+                    const int at = pk_value_byte(HP, BITS, r, d1 + i, &bit);
+                    element(i, (uint32_t)(uint8_t)b[at] >> bit);
+                }
+            } else {
+                const uint32_t *const k = words + (pk_key_byte(HP, BITS, r, d1, &bit) >> 2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    element(i, BITS == 8 ? k[i >> 2] >> (8 * (i & 3)) : k[0] >> (16 * (i & 1) + 4 * (i >> 1)));
             }
             pk_store8(row, d1, hd, vec, x);
         }
     } else {
         float x[2][8];
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-            if (mine) pk_load8(row, d0 + 16 * q, hd, vec, x[q]);
-            else
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[q][i] = 0.f;
+        for (int i = 0; i < 16; ++i) x[i >> 3][i & 7] = 0.f;
+        if (mine) pk_load16(row, d0, hd, vec, x);
         // the reductions keep a NaN (v_minimum3 / v_maximum3)
         float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
@@ -432,13 +447,21 @@ hipError_t launch_packed_copy(bool bf16, int bits, bool unpack, const PackedTabl
         const dim3 grid((n_units + units - 1) / units, std::min(planes - p0, 32768));
         pk_with_words(t, n_docs, [&](const auto &words) {
             constexpr int N = sizeof(words) / 4;
-#define KVR_COPY(T, HP, BITS, UN) \
-    kvr_launch((packed_copy_kernel<T, HP, BITS, UN, N>), grid, dim3(256), 0, s, words, n_docs, n_units, hd, Hkv, p0)
+#define KVR_COPY(T, HP, BITS, UN)                                                                                              \
+    if (hd == HP)                                                                                                              \
+        kvr_launch((packed_copy_kernel<T, HP, BITS, UN, true, N>), grid, dim3(256), 0, s, words, n_docs, n_units, hd, Hkv, p0); \
+    else                                                                                                                       \
+        kvr_launch((packed_copy_kernel<T, HP, BITS, UN, false, N>), grid, dim3(256), 0, s, words, n_docs, n_units, hd, Hkv, p0)
 #define KVR_CALL(HP, BITS)                                   \
-    if (bf16 && unpack) KVR_COPY(bf16_t, HP, BITS, true);    \
-    else if (bf16) KVR_COPY(bf16_t, HP, BITS, false);        \
-    else if (unpack) KVR_COPY(float, HP, BITS, true);        \
-    else KVR_COPY(float, HP, BITS, false)
+    if (bf16 && unpack) {                                    \
+        KVR_COPY(bf16_t, HP, BITS, true);                    \
+    } else if (bf16) {                                       \
+        KVR_COPY(bf16_t, HP, BITS, false);                   \
+    } else if (unpack) {                                     \
+        KVR_COPY(float, HP, BITS, true);                     \
+    } else {                                                 \
+        KVR_COPY(float, HP, BITS, false);                    \
+    }
             KVR_PACKED_DISPATCH(hd, bits, KVR_CALL);
 #undef KVR_CALL
 #undef KVR_COPY
