@@ -21,15 +21,37 @@ namespace {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
-__device__ __forceinline__ float wave_min(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fminf(v, __shfl_xor(v, o, 64));
-    return v;
+// x of another lane of the 16 in a row, by a DPP control.
+template <int CTRL>
+__device__ __forceinline__ uint32_t row_lane(uint32_t x) {
+    return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+constexpr int ROR = 0x120;                                    // + n: the lane n further on
+constexpr int XOR1 = 0xb1, XOR2 = 0x4e, HALF_MIRROR = 0x141;  // of four lanes; 7 - l of eight
+// Smallest and largest value of a wavefront, for all of its lanes (of NaN they may be
+// anything).
+__device__ __forceinline__ void wave_minmax(float *lo, float *hi) {
+    auto with = [&](uint32_t l, uint32_t h) {
+        *lo = fminf(*lo, __uint_as_float(l));
+        *hi = fmaxf(*hi, __uint_as_float(h));
+    };
+    auto l = [&] { return __float_as_uint(*lo); };
+    auto h = [&] { return __float_as_uint(*hi); };
+    with(row_lane<ROR + 8>(l()), row_lane<ROR + 8>(h()));
+    with(row_lane<ROR + 4>(l()), row_lane<ROR + 4>(h()));
+    with(row_lane<ROR + 2>(l()), row_lane<ROR + 2>(h()));
+    with(row_lane<ROR + 1>(l()), row_lane<ROR + 1>(h()));
+    // the four rows: each swap leaves a lane's own value and the other row's
+    const auto l16 = __builtin_amdgcn_permlane16_swap(l(), l(), false, false);
+    const auto h16 = __builtin_amdgcn_permlane16_swap(h(), h(), false, false);
+    *lo = __uint_as_float(l16[0]);
+    *hi = __uint_as_float(h16[0]);
+    with(l16[1], h16[1]);
+    const auto l32 = __builtin_amdgcn_permlane32_swap(l(), l(), false, false);
+    const auto h32 = __builtin_amdgcn_permlane32_swap(h(), h(), false, false);
+    *lo = __uint_as_float(l32[0]);
+    *hi = __uint_as_float(h32[0]);
+    with(l32[1], h32[1]);
 }
 
 // Scale and offset of a group of values within [lo, hi] (not `good`, or lo or hi not
@@ -71,21 +93,25 @@ __device__ __forceinline__ void write_row(const float x[2], int hd, bool value, 
         const int d = g * PK_GROUP + lane;
         const bool real = d < hd;
         const bool good = __ballot(real && !isfinite(x[g])) == 0;
-        float off, inv;
-        const uint32_t word = group_word<BITS>(wave_min(real ? x[g] : INFINITY), wave_max(real ? x[g] : -INFINITY), good,
-                                               &off, &inv);
+        float lo = real ? x[g] : INFINITY, hi = real ? x[g] : -INFINITY, off, inv;
+        wave_minmax(&lo, &hi);
+        const uint32_t word = group_word<BITS>(lo, hi, good, &off, &inv);
         uint32_t c = real && inv != 0.f ? (uint32_t)code_of(x[g], off, inv) : 0;
         int bit;
         if (value) {
             const int at = pk_value_byte(HP, BITS, r, d, &bit);
-            if (BITS == 4) c = (c | (__shfl_xor(c, 16, 64) << 4)) & 0xffu;
+            if (BITS == 4) {  // with the next 16 lanes' codes
+                const auto rows = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+                c = rows[0] | rows[1] << 4;
+            }
             if (BITS == 8 || !(lane & 16)) block[at] = (char)c;
         } else {
             // the lanes of a word put their codes together
             const int at = pk_key_byte(HP, BITS, r, d, &bit);
             c <<= 8 * (at & 3) + bit;
-#pragma unroll
-            for (int o = 1; o < 32 / BITS; o *= 2) c |= __shfl_xor(c, o, 64);
+            c |= row_lane<XOR1>(c);
+            c |= row_lane<XOR2>(c);
+            if (BITS == 4) c |= row_lane<HALF_MIRROR>(c);
             if ((lane & (32 / BITS - 1)) == 0) *reinterpret_cast<uint32_t *>(block + (at & ~3)) = c;
         }
         if (lane == 0) *reinterpret_cast<uint32_t *>(block + pk_code_bytes(HP, BITS) + (r * GS + g) * 4) = word;
@@ -93,7 +119,8 @@ __device__ __forceinline__ void write_row(const float x[2], int hd, bool value, 
 }
 
 // One wavefront per (row, plane): fresh rows of one layer.  Bound by its start and one
-// round of loads: 64 rows of 8 heads 4.2 us, 528 rows of 4 heads 5.4 us.
+// round of loads: 64 rows of 8 heads 3.8 us, 528 rows of 4 heads 5.2 us (4.2 and 5.4 with
+// exchanges between lanes through LDS).
 template <typename T, int HP, int BITS, int N>
 __global__ __launch_bounds__(256) void packed_append_kernel(PackedWords<N> t, int n_docs, const T *k, const T *v,
                                                             int64_t stride, int layer, int Hkv, int hd) {
@@ -120,10 +147,10 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedWords<N> t, in
 // packed block is put together (or taken apart) in LDS and moves to and from memory
 // in one contiguous piece; where only some positions are listed, their words and
 // bytes move one by one and the others are not touched.  Bound by memory: 32 layers of 8
-// heads, 5000 positions, 4 bits (839 MB) 159 us packed and 139 us read back, 5.3 and
-// 6.0 TB/s (a large copy 4.9: the packed cache is partly in the last-level cache); with
-// loads that wait for each other and masks for partial rows it was 192 and 178.  By one row a wavefront, straight to memory, the two took
-// 1960 us.
+// heads, 5000 positions, 4 bits (839 MB) 155 us packed and 138 us read back, 5.4 and
+// 6.1 TB/s (a large copy 4.9; the packed cache is partly in the last-level cache).  With
+// loads that wait for each other and masks for partial rows it was 192 and 178; by one
+// row a wavefront, straight to memory, the two took 1960 us.
 struct PackedUnit {
     char *block;     // the packed block
     size_t row;      // index of the block's first position among the cache's rows
