@@ -448,6 +448,9 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
                 s[h][i] = MASKED && key0 + 16 * CL * h + i >= limit ? -INFINITY : v;
             }
         }
+        // what uses a block's words stands before the next one's loads: no copies of registers
+#pragma unroll
+        for (int h = 0; h < H; ++h) asm volatile("" : "+v"(s[h]));
         if (more) load_keys(b + kw * SB);
         // the columns' probabilities, in place
         float mx = -INFINITY;
@@ -524,6 +527,8 @@ __global__ __launch_bounds__(64 * PK_WAVES_MAX) void attention_packed_kernel(Pac
                 }
             }
         }
+#pragma unroll
+        for (int g = 0; g < GS; ++g) asm volatile("" : "+v"(z[g]));
         if (more) load_values(b + kw * SB);
     };
     int b = b0;

@@ -644,15 +644,17 @@ struct PackedPlan {
 //
 // The estimate counts a wavefront's steps (1.5 us where all wavefronts are busy): the
 // longest block; if there are more blocks than a device holds, rounds of them if they
-// are alike, otherwise a device's share of all and a quarter of a last one; two steps
-// for a block's start and end, five for the launches, and the partials' way to memory
-// and back.  It comes within a sixth of most measured calls with many columns.
+// are alike, otherwise a device's share of all and a quarter of a last one; with few
+// columns the time that reading the caches takes, if that is longer; two steps for a
+// block's start and end, five for a launch, three for a combine, and the partials' way
+// to memory and back.  It comes within a sixth of most measured calls with many columns.
 hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<PackedSize> &size, PackedShape sh, PackedPlan *out) {
     const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads, cols = pk_cols(sh), sb = sh.copies == 4 ? 2 : 1;
     const int kw = sh.rows ? 1 : sh.waves / sh.cw;
-    long long units = 0, whole = 1;
+    long long units = 0, whole = 1, most_cols = 0;
     double work = 0;
     for (const PackedSize &z : size) {
+        most_cols = std::max(most_cols, z.cols);
         const long long ncg = (z.cols + cols - 1) / cols;
         units += ncg * Hkv * pk_blocks(z.keys);
         work += ncg * Hkv * z.mean;
@@ -680,31 +682,34 @@ hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<P
     const long long per_row = (G + cols - 1) / cols + 1;  // column groups that a row can touch
     while (range < whole && (whole + range - 1) / range * per_row > slots) range = std::min(whole, range * 2);
     // steps of a block of keys: the kernel for many rows goes through one in 2.2 us (1.6 with
-    // 64 dimensions), 8-bit codes cost a fifth more where they are used as they are, and two
-    // column tiles read the keys twice as often as four
+    // 64 dimensions), 8-bit codes cost a fifth more where they are used as they are, two
+    // column tiles read the keys twice as often as four, and four copies go through two
+    // blocks in one longer step
     const bool wide = pk_width(c->d.head_dim) == 128;
-    const double step = sh.rows ? (wide ? 1.45 : 1.05) : (bits == 8 && wide ? 1.2 : 1.0) * (sh.cw == 2 ? 1.06 : 1.0) / (kw * sb);
+    const double step = sh.rows ? (wide ? 1.45 : 1.05) : (bits == 8 && wide ? 1.2 : 1.0) * (sh.cw == 2 ? 1.06 : sh.copies == 4 ? 1.3 : 1.0) / (kw * sb);
     const bool even = work >= 0.9 * PK_BLOCK * units;  // (a prompt's blocks are not)
+    const double read = work / PK_BLOCK * 2 * pk_block_bytes(pk_width(c->d.head_dim), bits) / 7.3e6;  // (4.9 TB/s)
     auto estimate = [&](long long range) {
         const double n = (double)count(range), one = range * step + 2;
-        double steps = 5 + (n <= target ? one : even ? std::ceil(n / target) * one : (work / PK_BLOCK * step + 2 * n) / target + one / 4);
+        double steps = n <= target ? one : even ? std::ceil(n / target) * one : (work / PK_BLOCK * step + 2 * n) / target + one / 4;
+        if (most_cols <= 16) steps = std::max(steps, read);
         if (range < whole) {
             double bytes = 0;  // of partials
             for (const PackedSize &z : size)
                 bytes += (double)z.cols * Hkv * ((pk_blocks(z.keys) + range - 1) / range) * pk_part_row(c->d.head_dim) * 4;
-            steps += 2 * bytes / 6.7e6;  // (4.5 TB/s)
+            steps += 3 + 2 * bytes / 6.7e6;  // (4.5 TB/s)
         }
-        return steps;
+        return 5 + steps;
     };
     *out = PackedPlan{sh, range, estimate(range)};
-    // More blocks than that can still be faster: a last round that is part empty is shorter.
-    if (sh.cw > 1)
-        for (int k = 2; k <= 4; ++k) {
-            const long long r = (whole + k - 1) / k;
-            if (r >= range || r < 4 * least || k * per_row > slots) break;
-            const double steps = estimate(r);
-            if (steps < 0.95 * out->steps) *out = PackedPlan{sh, r, steps};
-        }
+    // No split can be as fast (64 documents, 384 blocks: 80 us, in 768 blocks 87), and so can
+    // be more blocks than the device holds, whose last round is part empty.
+    for (int k = 1; k <= 4; ++k) {
+        const long long r = (whole + k - 1) / k;
+        if (k > 1 && (most_cols <= 16 || r >= range || r < 4 * least || k * per_row > slots)) break;
+        const double steps = estimate(r);
+        if (steps < (k == 1 ? 1.0 : 0.95) * out->steps) *out = PackedPlan{sh, r, steps};
+    }
     return hipSuccess;
 }
 
