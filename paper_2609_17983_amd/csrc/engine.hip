@@ -725,8 +725,9 @@ hipError_t plan_documents(const kvr_ctx *c, int bits, bool pair, const std::vect
     if (most <= 16) {
         PackedShape sh{1, 1, 8, false};
         // Little work takes blocks of eight wavefronts, whose partials are fewer (one
-        // document of 40001 positions 17.5, blocks of four 18.7); much work blocks of four,
-        // which come out more even (64 documents 80 and 90).
+        // document of 40001 positions 17.5 us, blocks of four 18.7); much work, six steps for
+        // each wavefront of 768 blocks of four, takes those, which come out more even (64
+        // documents 80 and 90).
         sh.copies = most <= 4 ? 4 : most <= 8 ? 2 : 1;
         if (units >= 6ll * 768 * 4 * (sh.copies == 4 ? 2 : 1)) sh.waves = 4;
         return plan_shape(c, bits, pair, size, sh, out);
