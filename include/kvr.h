@@ -35,8 +35,9 @@
  *   must have been allocated by an earlier call.
  * - Arguments are validated before anything is enqueued: on any status other
  *   than KVR_OK or KVR_E_HIP, no GPU work was enqueued and no cache was
- *   touched.  KVR_E_HIP means a HIP call failed after enqueueing began; cache
- *   contents are then undefined.  kvr_last_error() describes the failure.
+ *   touched.  KVR_E_HIP means a HIP call failed, or host memory ran out, after
+ *   enqueueing began; cache contents are then undefined.  kvr_last_error()
+ *   describes the failure.
  *
  * Data layouts
  * - Weights: dtype of kvr_dims.dtype (fp32 or bf16), row-major.  Linear

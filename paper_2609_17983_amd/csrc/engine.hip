@@ -34,8 +34,17 @@ LaunchTimer &launch_timer() {
     return t;
 }
 
+// What a plan of attention over packed caches looks at of a document: its
+// columns, and the keys that a row sees at most and on average.
+struct PackedSize {
+    long long cols;
+    int keys;
+    double mean;
+};
+
 // The host tables of one pass.  A context keeps one set, reserved to its
-// capacities when it is created, so that planning a pass allocates nothing.
+// capacities when it is created, so that planning a pass allocates nothing;
+// the lists of packed passes grow with the first calls and keep their memory.
 struct Tables {
     struct Block { int doc, row0, nrows, kmax; };  // attention row block (planner)
     std::vector<RowInfo> rows;
@@ -52,6 +61,7 @@ struct Tables {
         int splits;  // largest number of key ranges
     };
     std::vector<PackedLaunch> packed;
+    std::vector<PackedSize> sizes, part;  // its plan's: the documents, and one of two parts of them
     int att_mt = 1;  // 16-row tiles per attention item (rows of a row block / 16)
     void clear() {
         rows.clear(); docs.clear(); items.clear(); comb.clear(); blocks.clear(); packed.clear();
@@ -115,6 +125,7 @@ struct kvr_ctx {
     char *d_tables = nullptr;
     size_t tables_bytes = 0;
     Tables tab;  // host tables of the pass being planned (capacity reserved at create)
+    bool enqueued = false;  // by the call that is running (guarded)
     void *scratch_ptr = nullptr;        // this device's copy of `scratch` (kvr_select_attention_noalloc)
     hipError_t scratch_err = hipSuccess;
 
@@ -620,14 +631,6 @@ struct PackedQuery {
     const int32_t *pos;
     int step;
 };
-// What a plan looks at of a document: its columns, and the keys that a row sees at most
-// and on average.
-struct PackedSize {
-    long long cols;
-    int keys;
-    double mean;
-};
-
 // How the attention of some documents is launched, and its estimated time.
 struct PackedPlan {
     PackedShape sh;
@@ -756,7 +759,8 @@ template <typename DocAt>
 hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_docs, DocAt doc, bool row_table) {
     const int G = c->d.n_heads / c->d.n_kv_heads, Hkv = c->d.n_kv_heads;
     t.packed.clear();
-    std::vector<PackedSize> size(n_docs), part[2];
+    std::vector<PackedSize> &size = t.sizes, &part = t.part;
+    size.resize(n_docs);
     int few = 0, many = 0;
     for (int i = 0; i < n_docs; ++i) {
         const PackedQuery q = doc(i);
@@ -779,10 +783,10 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
     if (err == hipSuccess && few > 0 && many > 0) {
         PackedPlan apart[2];
         for (int p = 0; p < 2 && err == hipSuccess; ++p) {
-            part[p] = size;
-            for (PackedSize &z : part[p])
+            part = size;
+            for (PackedSize &z : part)
                 if ((z.cols > 16) != (p == 0)) z.cols = 0;
-            err = plan_documents(c, bits, pair, part[p], &apart[p]);
+            err = plan_documents(c, bits, pair, part, &apart[p]);
         }
         if (err == hipSuccess && apart[0].steps + apart[1].steps < plan[0].steps) {
             parts = 2;
@@ -905,6 +909,7 @@ kvr_status run_pass(kvr_ctx *c, Tables &t, hipStream_t s, int kv_layer = -1, con
     // not read the staging buffer, which the context's next call overwrites:
     // its tables go into the graph as kernel arguments.
     const bool captured = capturing(s);
+    c->enqueued = true;
     const bool by_kernel = !captured && total <= UPLOAD_BY_KERNEL;
     if (captured) {
         TableChunk chunk;
@@ -1210,14 +1215,17 @@ kvr_status check_dims(const kvr_dims *d) {
     return KVR_OK;
 }
 
-// Runs the body of an entry point; what it throws (host memory) becomes a status.
+// Runs the body of an entry point; what it throws (host memory) becomes a status:
+// KVR_E_NOMEM says that nothing was enqueued, which a call of several passes may have
+// done by then.
 template <typename Body>
 kvr_status guarded(kvr_ctx *c, Body body) {
+    if (c) c->enqueued = false;
     try {
         return body();
     } catch (...) {
-        if (c) c->err.clear();  // no memory for a message
-        return KVR_E_NOMEM;
+        if (c) c->err = "out of memory";  // (short enough to need none)
+        return c && c->enqueued ? KVR_E_HIP : KVR_E_NOMEM;
     }
 }
 
