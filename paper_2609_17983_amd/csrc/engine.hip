@@ -82,7 +82,7 @@ static __device__ __align__(256) unsigned char scratch[NOALLOC_SCRATCH_BYTES];
 
 struct kvr_ctx {
     kvr_dims d{};
-    int device = 0;
+    int device = 0, units = 0;  // and its compute units
     bool bf16 = true;
     bool force_simple = false;
     std::vector<kvr_layer_weights> layers;
@@ -673,10 +673,11 @@ hipError_t plan_shape(const kvr_ctx *c, int bits, bool pair, const std::vector<P
     PackedAttnArgs probe{};
     probe.hd = c->d.head_dim;
     probe.q_lo = pair ? c->Qb_lo : nullptr;
-    int target = 0;
+    int per_unit = 0;
     static const PackedTable none{};
-    const hipError_t err = launch_attention_packed(c->bf16, bits, sh, none, probe, nullptr, &target);
+    const hipError_t err = launch_attention_packed(c->bf16, bits, sh, none, probe, nullptr, &per_unit);
     if (err != hipSuccess) return err;
+    const int target = c->units * per_unit;
     const long long least = sh.rows ? 4 : kw * sb;
     long long range = std::max<long long>(least, (units + target - 1) / target);
     range = whole <= 2 * least ? whole : std::min(whole, (range + sb - 1) / sb * sb);
@@ -1289,6 +1290,7 @@ kvr_status kvr_create(const kvr_dims *dims, const kvr_weights *wts, kvr_ctx **ou
     c->final_norm = wts->final_norm;
     c->lm_head = wts->lm_head ? wts->lm_head : wts->embed;
     hipError_t e = hipGetDevice(&c->device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&c->units, hipDeviceAttributeMultiprocessorCount, c->device);
     if (e != hipSuccess) { delete c; return hip_fail(nullptr, e, "hipGetDevice"); }
     // the no-allocation selector's scratch on this (current) device; a failed
     // lookup only disables that entry point

@@ -145,21 +145,18 @@ constexpr int pk_cols(PackedShape s) { return 16 / s.copies * s.cw * (s.rows ? P
 constexpr int PK_WAVES_MAX = 8;
 constexpr int pk_part_row(int hd) { return pk_width(hd) + 4; }
 // resident given: nothing is launched, and it receives the number of blocks that a
-// device holds at a time (only hd and q_lo of `a` are looked at).
+// compute unit holds at a time (only hd and q_lo of `a` are looked at).
 hipError_t launch_attention_packed(bool bf16, int bits, PackedShape sh, const PackedTable &t, const PackedAttnArgs &a,
                                    hipStream_t s, int *resident = nullptr);
-// The number of blocks of `waves` wavefronts with `lds` bytes that a device holds at a
-// time.  `known`: the answers so far, by waves / 4 - 1.
+// The number of blocks of `waves` wavefronts with `lds` bytes that a compute unit holds
+// at a time, the same on every device.  `known`: the answers so far, by waves / 4 - 1.
 template <typename K>
 inline hipError_t pk_resident(K kernel, int waves, size_t lds, std::atomic<int> *known, int *resident) {
     int n = known[waves / 4 - 1].load(std::memory_order_relaxed);
     if (n == 0) {
-        int dev = 0, units = 0, blocks = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e == hipSuccess) e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, dev);
-        if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, 64 * waves, lds);
+        const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, 64 * waves, lds);
         if (e != hipSuccess) return e;
-        n = units * (blocks > 0 ? blocks : 1);
+        if (n < 1) n = 1;
         known[waves / 4 - 1].store(n, std::memory_order_relaxed);
     }
     *resident = n;

@@ -47,3 +47,20 @@ def test_planning_again_allocates_nothing():
     """A generation's later passes plan in the memory of its first ones."""
     *failures, last = run(SHORT_OF_MEMORY + "result = outcomes(lambda c: kvr.kvr_generate_packed(c, P, 4, 10, 100, P, 3, 5))")
     assert last[0] == kvr.KVR_OK and all(launches == 0 for _, launches in failures)
+
+
+@pytest.mark.parametrize("rows", [1, 48])
+def test_key_ranges_are_for_the_contexts_device(rows):
+    """Which device a process asked first has no say in another device's plans."""
+    body = """
+    host.host_units(1, 32)
+    grids = []
+    for device in %s:
+        host.hipSetDevice(device)
+        c = context(dims(max_ctx=8000))
+        host.hipSetDevice(0)  # (a call works on its context's device)
+        grids.append(attend(c, 4, [(8000, list(range(8000 - %d, 8000)))])[0]["grid"])
+    result = grids
+    """
+    both, one, other = (run(body % (devices, rows)) for devices in ((0, 1), (0,), (1,)))
+    assert both == one + other and one != other
