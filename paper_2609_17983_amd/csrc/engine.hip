@@ -540,10 +540,10 @@ struct TableFill {
     }
     // An entry for the first rows of a list of n positions (`step` words apart):
     // returns how many, 0 when the table is full.  A run of consecutive positions
-    // needs no list; one of an entry's length or more gets an entry of its own if
-    // `runs`, and the whole list is one entry that reads the pass's row table if
-    // `row_table`.
-    int add(const void *packed, int blocks, int row0, const int32_t *pos, int step, int n, bool runs, bool row_table) {
+    // needs no list; one of `least` or more gets an entry of its own (0: only the
+    // whole list), and the whole list is one entry that reads the pass's row table
+    // if `row_table`.
+    int add(const void *packed, int blocks, int row0, const int32_t *pos, int step, int n, int least, bool row_table) {
         const int room = tail - (docs + 1) * PK_ENTRY;
         if (room < 0) return 0;
         auto run = [&](int i) {  // length of the run that starts at i
@@ -553,18 +553,18 @@ struct TableFill {
         };
         int k = run(0);
         uint32_t ref = PK_RUN;
-        if (k < n && !(runs && k >= PK_ENTRY)) {
+        if (k < n && !(least > 0 && k >= least)) {
             if (row_table) {
                 ref = PK_ROWS;
                 k = n;
             } else {
-                int last = k;
+                int last = least > 0 ? k : n;
                 while (last < n && last < room) {
                     const int more = run(last);
-                    if (runs && more >= PK_ENTRY) break;
+                    if (more >= least) break;
                     last += more;
                 }
-                k = std::min(std::min(last, n), room);
+                k = std::min(last, room);
                 if (k < 1) return 0;
                 ref = take(k);
                 for (int i = 0; i < k; ++i) t->words.w[tail + i] = (uint32_t)pos[(size_t)i * step];
@@ -802,6 +802,14 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
         const PackedShape sh = plan[p].sh;
         const long long range = plan[p].range, cols = pk_cols(sh);
         const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
+        // An entry's last column group is part empty, so a document's rows are one entry,
+        // listed, unless the lists fill more than one table: runs of four column groups or
+        // more are then taken out of them, which costs a fifth more groups at most and saves
+        // launches (5000 consecutive rows and a repeated one: one launch, six without).
+        long long words = 0;
+        for (int i = 0; i < n_docs; ++i)
+            if (parts == 1 || (size[i].cols > 16) == (p == 0)) words += PK_ENTRY + size[i].cols / G;
+        const int least = words > PK_WORDS ? std::max<int>(PK_ENTRY, (int)((4 * cols + G - 1) / G)) : 0;
         TableFill fill(nullptr);
         int used = 0;  // partial slots of the launch
         auto open = [&] {
@@ -826,7 +834,7 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
                 fit = std::min<long long>(fit, q.n);
                 if (ns > 1) fit = std::min(fit, (slots - used) / ns * cols / G);
                 const int before = fill.docs;
-                const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, false, row_table);
+                const int n = fit < 1 ? 0 : fill.add(q.packed, pk_blocks(q.n_cap), q.row0, q.pos, q.step, (int)fit, least, row_table);
                 if (n == 0) {
                     open();
                     continue;
@@ -2000,7 +2008,7 @@ static kvr_status append_packed(kvr_ctx *c, int32_t layer, int32_t bits, const k
         const kvr_packed_rows &dc = docs[i];
         for (int done = 0; done < dc.n_rows;) {
             const int most = std::min(dc.n_rows - done, PK_MAX_GRID - (row - first));
-            const int n = most < 1 ? 0 : fill.add(dc.d_packed, pk_blocks(dc.n_cap), row, dc.h_positions + done, 1, most, true, false);
+            const int n = most < 1 ? 0 : fill.add(dc.d_packed, pk_blocks(dc.n_cap), row, dc.h_positions + done, 1, most, PK_ENTRY, false);
             if (n == 0) {
                 const hipError_t e = flush();
                 if (e != hipSuccess) return hip_fail(c, e, who);

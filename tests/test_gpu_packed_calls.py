@@ -1,0 +1,114 @@
+"""Calls over packed caches that test_gpu_packed.py does not make, against the same reference, with the kernels that a call
+launched read from a captured copy of it."""
+import ctypes
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_17983_amd as kvr
+from tests import packed_ref as ref
+from tests.gpu_util import TOL, say
+from tests.test_gpu_packed import BF16, F32, TDT, Ctx, fill, rows_like, stream
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------- what a call launched
+
+
+class _Dim3(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_uint), ("y", ctypes.c_uint), ("z", ctypes.c_uint)]
+
+
+class _KernelNode(ctypes.Structure):
+    _fields_ = [("block", _Dim3), ("extra", ctypes.c_void_p), ("func", ctypes.c_void_p), ("grid", _Dim3),
+                ("params", ctypes.c_void_p), ("lds", ctypes.c_uint)]
+
+
+def launched(call):
+    """The packed-attention kernels of a call (captured, not run): (name, template arguments, threads of a block)."""
+    hip = ctypes.CDLL("libamdhip64.so")
+    hip.hipKernelNameRefByPtr.restype = ctypes.c_char_p
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(g):
+        call()
+    raw, n = ctypes.c_void_p(g.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert hip.hipGraphGetNodes(raw, None, ctypes.byref(n)) == 0
+    nodes = (ctypes.c_void_p * n.value)()
+    assert hip.hipGraphGetNodes(raw, nodes, ctypes.byref(n)) == 0
+    out = []
+    for node in nodes:
+        p = _KernelNode()
+        if hip.hipGraphKernelNodeGetParams(ctypes.c_void_p(node), ctypes.byref(p)) != 0:
+            continue  # no kernel
+        name = hip.hipKernelNameRefByPtr(ctypes.c_void_p(p.func), None).decode()
+        m = re.search(r"(attention_packed\w*?_kernel)I([tf]?)((?:Li\d+E)+)E", name)
+        if m and "combine" not in m[1]:
+            out.append((m[1], m[2], tuple(int(x) for x in re.findall(r"Li(\d+)E", m[3])), p.block.x))
+    return out
+
+
+# ---------------------------------------------------------------------------- attention
+
+
+class Case:
+    """Query rows over packed caches, and what they should give."""
+
+    def __init__(self, c, bits, docs, packs, decs, seed=0, spoil=False):
+        """docs: (index into packs, positions).  spoil: rows at -1 hold NaN."""
+        self.bits, self.docs, self.dtype = bits, docs, c.dtype
+        R = sum(len(p) for _, p in docs)
+        self.x, t = rows_like((R, c.Hq * c.hd), c.dtype, seed + 77)
+        if spoil:
+            t[[p < 0 for _, d in docs for p in d]] = float("nan")
+        self.q, self.packs = t.cuda(), [p.cuda() for p in packs]
+        self.want, self.bound = np.zeros((2, R, c.Hq, c.hd)), np.zeros((2, R, c.Hq))
+        self.want = self.want[0]
+        half = torch.finfo(TDT[c.dtype]).eps / 2
+        at = 0
+        for i, pos in docs:
+            q = self.x[at:at + len(pos)].reshape(-1, c.Hq, c.hd)
+            self.want[at:at + len(pos)] = ref.attend(q, pos, ref.values(*decs[i][0]), ref.values(*decs[i][1]))
+            for pairs in (0, 1):
+                self.bound[pairs, at:at + len(pos)] = ref.attend_bound(q, pos, *decs[i], bits, c.dtype == F32, pairs == 1)
+            at += len(pos)
+        self.tol = self.bound[..., None] * (1 + half) + half * np.abs(self.want) + 1e-30
+
+    def call(self, c, out):
+        lst = kvr.make_packed_rows([(self.packs[i].data_ptr(), self.packs[i].shape[3] * 32, p) for i, p in self.docs])
+        n = c.Hq * c.hd
+        return lambda: kvr.kvr_attention_packed(c.ctx, c.layers - 1, self.bits, lst, self.q.data_ptr(), n, out.data_ptr(), n,
+                                                stream())
+
+    def check(self, c, kernel=None, tag=""):
+        """Runs the call and holds it to the bound of the kernel that it launched; kernel: the name and block that it has to
+        be.  Returns the output."""
+        out = torch.full((self.q.shape[0], c.Hq * c.hd), 3.0, dtype=TDT[c.dtype], device="cuda")
+        call = self.call(c, out)
+        call()
+        torch.cuda.synchronize()
+        ran = launched(call)
+        if kernel:
+            assert {(k[0], k[3]) for k in ran} == {kernel}, ran
+        y = out.cpu().float().numpy().reshape(self.want.shape).astype(np.float64)
+        off = np.abs(y - self.want) / self.tol[int(any("rows" in k[0] for k in ran))]
+        say(f"attention {tag} {sorted(set(ran))}: worst error over bound {np.nanmax(off):.3f}")
+        assert np.array_equal(np.isnan(y), np.isnan(self.want)) and np.nanmax(off) <= 1.0
+        # and over all of them: the output's rounding alone in bf16, the repository's tolerance in fp32
+        ok = np.isfinite(self.want)
+        rel = np.linalg.norm(y[ok] - self.want[ok]) / np.linalg.norm(self.want[ok])
+        assert rel <= (TOL[F32] if c.dtype == F32 else torch.finfo(TDT[c.dtype]).eps / 2)
+        return out
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,bits", [(BF16, 8, 2, 64, 4), (BF16, 32, 8, 128, 8), (F32, 4, 4, 64, 8)])
+def test_consecutive_rows_with_others(dtype, Hq, Hkv, hd, bits):
+    """Runs and short pieces of a list that no table holds whole: every row lands where it belongs."""
+    with Ctx(dtype, Hq, Hkv, hd, max_ctx=1152) as c:
+        packs, decs = zip(*[fill(c, n, bits, n) for n in (1100, 60)])
+        docs = [(1, [59, 3]), (0, [7, -1] + list(range(30, 700)) + [5] + list(range(0, 600, 5)) + list(range(800, 1100))),
+                (1, list(range(60)))]
+        case = Case(c, bits, docs, packs, decs)
+        case.check(c, tag="runs")

@@ -49,18 +49,43 @@ def test_planning_again_allocates_nothing():
     assert last[0] == kvr.KVR_OK and all(launches == 0 for _, launches in failures)
 
 
-@pytest.mark.parametrize("rows", [1, 48])
-def test_key_ranges_are_for_the_contexts_device(rows):
+def test_key_ranges_are_for_the_contexts_device():
     """Which device a process asked first has no say in another device's plans."""
     body = """
     host.host_units(1, 32)
-    grids = []
+    result = []
     for device in %s:
         host.hipSetDevice(device)
         c = context(dims(max_ctx=8000))
         host.hipSetDevice(0)  # (a call works on its context's device)
-        grids.append(attend(c, 4, [(8000, list(range(8000 - %d, 8000)))])[0]["grid"])
-    result = grids
+        result.append([attend(c, 4, [(8000, list(range(8000 - rows, 8000)))])[0]["grid"] for rows in (1, 48)])
     """
-    both, one, other = (run(body % (devices, rows)) for devices in ((0, 1), (0,), (1,)))
-    assert both == one + other and one != other
+    both, one, other = (run(body % devices) for devices in ("(0, 1)", "(0,)", "(1,)"))
+    assert both == one + other
+    assert all(a != b for a, b in zip(*both))
+
+
+def test_consecutive_rows_with_others_are_one_launch():
+    """A prompt beside idle, repeated or further rows takes as few launches as alone."""
+    alone, *rest = run("""
+    c = context(dims(max_ctx=8000, max_rows=1))
+    prompt = list(range(5000))
+    result = [attend(c, 4, [(8000, prompt)])]
+    for extra in ([7], [-1, -1], [3, 900, 40], list(range(100, 140))):
+        result += [attend(c, 4, [(8000, extra + prompt)]), attend(c, 4, [(8000, prompt + extra)])]
+    """)
+    for launches in rest:
+        assert len(launches) == len(alone) == 1 and launches[0]["name"] == alone[0]["name"]
+        # (32 heads of 8, columns by 256: at most a group more for each piece)
+        assert alone[0]["grid"][1] <= launches[0]["grid"][1] <= alone[0]["grid"][1] + 3
+
+
+def test_scattered_rows_are_one_entry():
+    """Rows that a table holds are not cut at their runs, whose last column groups would be part empty."""
+    launches = run("""
+    c = context(dims(max_ctx=8000, max_rows=1))
+    result = attend(c, 4, [(8000, [40 * i + j for i in range(40) for j in range(13)])])
+    """)
+    assert len(launches) <= 2  # (a combine, if the keys are split)
+    # 520 rows of four heads in groups of 32, 64 or 256 columns; by runs they were 80 or 40 groups
+    assert any(launches[0]["grid"][1] % -(-520 * 4 // cols) == 0 for cols in (32, 64, 256))
