@@ -85,6 +85,7 @@ struct kvr_ctx {
     int device = 0, units = 0;  // and its compute units
     bool bf16 = true;
     bool force_simple = false;
+    PackedShape packed_shape{0, 0, 0, false};  // KVR_PACKED_SHAPE (waves 0: not set)
     std::vector<kvr_layer_weights> layers;
     const void *embed = nullptr, *final_norm = nullptr;
 
@@ -726,6 +727,7 @@ hipError_t plan_documents(const kvr_ctx *c, int bits, bool pair, const std::vect
         if (z.cols > 0) units += (long long)Hkv * pk_blocks(z.keys);
     }
     *out = PackedPlan{};
+    if (c->packed_shape.waves > 0) return plan_shape(c, bits, pair, size, c->packed_shape, out);
     if (most <= 16) {
         PackedShape sh{1, 1, 8, false};
         // Little work takes blocks of eight wavefronts, whose partials are fewer (one
@@ -1293,6 +1295,11 @@ kvr_status kvr_create(const kvr_dims *dims, const kvr_weights *wts, kvr_ctx **ou
     c->bf16 = d.dtype == KVR_BF16;
     const char *fs = getenv("KVR_SIMPLE");
     c->force_simple = fs && fs[0] == '1';
+    // blocks of packed attention: column tiles, copies of the columns and wavefronts, a
+    // digit each (818: the kernel for many rows); others are not heeded
+    const int shape = env_int("KVR_PACKED_SHAPE", 0);
+    for (const int known : {114, 118, 124, 128, 144, 148, 218, 418, 818})
+        if (shape == known) c->packed_shape = {shape / 100, shape / 10 % 10, shape % 10, shape == 818};
     c->layers.assign(wts->layers, wts->layers + d.n_layers);
     c->embed = wts->embed;
     c->final_norm = wts->final_norm;

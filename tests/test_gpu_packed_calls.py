@@ -112,3 +112,35 @@ def test_consecutive_rows_with_others(dtype, Hq, Hkv, hd, bits):
                 (1, list(range(60)))]
         case = Case(c, bits, docs, packs, decs)
         case.check(c, tag="runs")
+
+
+SHAPES = {114: "attention_packed_kernel", 118: "attention_packed_kernel", 124: "attention_packed_kernel",
+          128: "attention_packed_kernel", 144: "attention_packed_kernel", 148: "attention_packed_kernel",
+          218: "attention_packed_kernel", 418: "attention_packed_kernel", 818: "attention_packed_rows_kernel"}
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,bits", [
+    (BF16, 8, 2, 128, 4), (BF16, 14, 2, 96, 8), (BF16, 12, 3, 64, 4), (BF16, 8, 2, 40, 8), (F32, 8, 2, 128, 4), (F32, 4, 2, 64, 8)])
+def test_attention_in_every_shape(dtype, Hq, Hkv, hd, bits, monkeypatch):
+    """Blocks of four and of eight wavefronts, copies of the columns, column tiles and the kernel for many rows, each made to
+    take single rows, several rows, split and unsplit keys, repeated and idle rows."""
+    with Ctx(dtype, Hq, Hkv, hd, layers=2, max_ctx=1184) as c:
+        packs, decs = zip(*[fill(c, n, bits, n, slots) for n, slots in ((1100, 1180), (33, 64), (300, 300))])
+        docs = [(0, [1099]), (1, [32]), (2, [299, -1, 16, 299]), (0, list(range(900, 948))), (1, [-1]), (2, [0])]
+        case = Case(c, bits, docs, packs, decs, spoil=True)
+    for shape, name in SHAPES.items():
+        if shape == 818 and dtype == F32:
+            continue
+        monkeypatch.setenv("KVR_PACKED_SHAPE", str(shape))
+        with Ctx(dtype, Hq, Hkv, hd, layers=2, max_ctx=1184) as c:
+            case.check(c, (name, 64 * (shape % 10)), str(shape))
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,bits,rows", [
+    (BF16, 32, 8, 128, 4, 120), (BF16, 28, 4, 128, 8, 120), (BF16, 32, 2, 64, 4, 240), (F32, 8, 8, 64, 8, 120)])
+def test_attention_of_a_large_batch_of_single_rows(dtype, Hq, Hkv, hd, bits, rows):
+    """Enough work for blocks of four wavefronts, and more documents than a table holds (they share a cache)."""
+    with Ctx(dtype, Hq, Hkv, hd, max_ctx=1536) as c:
+        pack, dec = fill(c, 1500, bits, 3)
+        docs = [(0, [-1 if i % 17 == 5 else 1499 - i % 40]) for i in range(rows)]
+        Case(c, bits, docs, [pack], [dec]).check(c, ("attention_packed_kernel", 256), "batch")

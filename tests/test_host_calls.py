@@ -89,3 +89,25 @@ def test_scattered_rows_are_one_entry():
     assert len(launches) <= 2  # (a combine, if the keys are split)
     # 520 rows of four heads in groups of 32, 64 or 256 columns; by runs they were 80 or 40 groups
     assert any(launches[0]["grid"][1] % -(-520 * 4 // cols) == 0 for cols in (32, 64, 256))
+
+
+def test_shapes_can_be_chosen():
+    """KVR_PACKED_SHAPE, read when a context is made: each form of the kernels; other numbers have no effect."""
+    got = run("""
+    import os
+    result = {}
+    for shape in (0, 114, 118, 124, 128, 144, 148, 218, 418, 818, 814, 999, 7):
+        os.environ["KVR_PACKED_SHAPE"] = str(shape)
+        c = context(dims(max_ctx=4096))
+        del os.environ["KVR_PACKED_SHAPE"]
+        result[shape] = [attend(c, 4, [(4096, [4000])])[0], attend(c, 8, [(4096, list(range(48)))])[0]]
+    """)
+    for shape, launches in got.items():
+        if shape in ("0", "814", "999", "7"):
+            assert launches == got["0"]
+            continue
+        for l, bits in zip(launches, (4, 8)):
+            assert l["threads"] == 64 * int(shape[2])
+            kernel = "attention_packed_rows_kernel<128, %d, 1>" if shape == "818" else \
+                "attention_packed_kernel<unsigned short, 128, %d, 1, " + shape[1] + ", 64>"
+            assert l["name"] == kernel % bits
