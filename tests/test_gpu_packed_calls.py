@@ -144,3 +144,59 @@ def test_attention_of_a_large_batch_of_single_rows(dtype, Hq, Hkv, hd, bits, row
         pack, dec = fill(c, 1500, bits, 3)
         docs = [(0, [-1 if i % 17 == 5 else 1499 - i % 40]) for i in range(rows)]
         Case(c, bits, docs, [pack], [dec]).check(c, ("attention_packed_kernel", 256), "batch")
+
+
+@pytest.mark.parametrize("shape", [0, 418, 818])
+def test_attention_beyond_32_bit_offsets(shape, monkeypatch):
+    """The last plane of a packed cache of more than 4 GiB: queries that find the first and the very last position among
+    200000, whose keys are zero elsewhere."""
+    monkeypatch.setenv("KVR_PACKED_SHAPE", str(shape))
+    layers, n, Hkv, hd = 17, 200000, 8, 128
+    with Ctx(BF16, Hkv, Hkv, hd, layers=layers, max_ctx=n) as c:
+        size = kvr.kvr_packed_bytes(c.dims, n, 8)
+        assert size > 1 << 32
+        dev = torch.zeros(size, dtype=torch.uint8, device="cuda")
+        pos = [0, 5, n - 1]
+        rng = np.random.default_rng(4)
+        t = torch.tensor(rng.standard_normal((2, 3, Hkv * hd)), dtype=torch.float32).bfloat16()
+        kv, x = t.cuda(), t.float().numpy()
+        docs = kvr.make_packed_rows([(dev.data_ptr(), n, pos)])
+        kvr.kvr_append_packed(c.ctx, layers - 1, 8, docs, kv.data_ptr(), kv.data_ptr() + 3 * Hkv * hd * 2, Hkv * hd, stream())
+        dec = []
+        for v in range(2):  # the written rows as slots 0, 5 and 63 of two blocks
+            p = np.zeros((Hkv, 2, ref.block_bytes(hd, 8)), np.uint8)
+            ref.write(p, x[v].reshape(3, Hkv, hd).transpose(1, 0, 2), [0, 5, 63], 8, v == 1)
+            dec.append(ref.read(p, 64, hd, 8, v == 1))
+        k, v = (ref.values(*d)[:, [0, 5, 63]] for d in dec)
+        # rows that look for the three positions, and one that looks for the last one and does not see it
+        seen = [n - 1, n - 1, n - 1, n - 2]
+        q = torch.tensor(4.0 * x[0][[0, 1, 2, 2]]).bfloat16()
+        qn = q.float().numpy().reshape(4, Hkv, hd)
+
+        def expect(visible):
+            """By the softmax over the written rows that are visible and the zero rows, whose scores and values are zero."""
+            want = np.zeros((4, Hkv, hd))
+            for r in range(4):
+                for h in range(Hkv):
+                    s = np.where(visible[r], qn[r, h].astype(np.float64) @ k[h].T / np.sqrt(hd), -np.inf)
+                    w = np.exp(s - s.max())
+                    want[r, h] = w @ v[h] / (w.sum() + (seen[r] + 1 - np.isfinite(s).sum()) * np.exp(-s.max()))
+            return want
+
+        see = np.array([[True, True, p == n - 1] for p in seen])
+        want = expect(see)
+        V = float((256 * dec[1][1].astype(np.float64) + np.abs(dec[1][2])).max())
+        # the bound over the written rows, and the sums over all slots
+        tol = ref.attend_bound(qn, [63] * 4, dec[0], dec[1], 8, False, shape == 818)[..., None] + \
+            2 * (n / 32) * 2.0 ** -24 * V + 2.0 ** -8 * np.abs(want)
+        without = see.copy()
+        without[:, 2] = False
+        for wrong in (expect(without), 0 * want, 2 * want):  # the bound sees what it is for
+            assert (np.abs(wrong - want)[2] > tol[2]).mean() > 0.9
+        dq, out = q.cuda(), torch.full((4, Hkv * hd), 3.0, dtype=torch.bfloat16, device="cuda")
+        rows = kvr.make_packed_rows([(dev.data_ptr(), n, seen)])
+        kvr.kvr_attention_packed(c.ctx, layers - 1, 8, rows, dq.data_ptr(), Hkv * hd, out.data_ptr(), Hkv * hd, stream())
+        torch.cuda.synchronize()
+        off = np.abs(out.cpu().double().numpy().reshape(want.shape) - want) / tol
+        say(f"beyond 32 bits, shape {shape}: worst error over bound {off.max():.3f}")
+        assert off.max() <= 1.0
