@@ -146,6 +146,53 @@ def test_attention_of_a_large_batch_of_single_rows(dtype, Hq, Hkv, hd, bits, row
         Case(c, bits, docs, [pack], [dec]).check(c, ("attention_packed_kernel", 256), "batch")
 
 
+def cancelling(p, n, hd, bits, monkeypatch):
+    """Fills the planes p [2][heads][blocks][bytes] of one layer: positions 2 i and 2 i + 1 have equal keys, and values
+    m + s c and -(m + s c); the last 16 add small ones.  Returns what ref.read gives."""
+    rng = np.random.default_rng(bits)
+    top, heads = (1 << bits) - 1, p.shape[1]
+    keys = np.repeat(0.3 * rng.standard_normal((heads, n // 2, hd)).astype(np.float32), 2, 1)
+    ref.write(p[0], keys, range(n), bits, False)
+    codes = rng.integers(0, top + 1, (heads, n // 2, hd))
+    codes = np.stack([codes, top - codes], 2).reshape(heads, n, hd)
+    scale = np.full((heads, n, hd // 64), 2.0 ** -bits, np.float32)
+    offset = np.tile(np.repeat(np.float32([-(top + 1) / 2, -(top - 1) / 2])[:, None], hd // 64, 1), (heads, n // 2, 1)) * scale
+    scale[:, -16:] *= 2.0 ** -9
+    offset[:, -16:] = 2.0 ** -9
+    with monkeypatch.context() as m:  # these codes, not what the format would make of some values
+        m.setattr(ref, "quantise", lambda *_: (codes, scale, offset.astype(np.float32)))
+        ref.write(p[1], np.zeros((heads, n, hd), np.float32), range(n), bits, True)
+    dec = [ref.read(p[kv], n, hd, bits, kv == 1) for kv in range(2)]
+    assert np.array_equal(dec[1][0], codes) and np.array_equal(dec[1][1], scale) and np.array_equal(dec[1][2], offset)
+    v = ref.values(*dec[1])[:, :-16].reshape(heads, -1, 2, hd)
+    assert (v[:, :, 0] == -v[:, :, 1]).all() and np.abs(v).max() > 0.4
+    return dec
+
+
+@pytest.mark.parametrize("shape", [148, 144, 418, 818])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_attention_of_values_that_cancel(bits, shape, monkeypatch):
+    """Outputs below 2^-11 of their terms: each value has its opposite under an equal key.  The pieces' rounding is part of
+    the largest value, as the bound states it, not of the output."""
+    monkeypatch.setenv("KVR_PACKED_SHAPE", str(shape))
+    n, hd = 512, 128
+    with Ctx(BF16, 8, 2, hd, max_ctx=n) as c:
+        p = c.packed(n, bits).numpy()
+        dec = cancelling(p[0], n, hd, bits, monkeypatch)
+        case = Case(c, bits, [(0, [n - 1] * 40)], [torch.tensor(p)], [dec])
+        terms = np.abs(ref.values(*dec[1])).max()
+        assert 0 < np.abs(case.want).max() < 2.0 ** -11 * terms
+        out = torch.zeros((40, 8 * hd), dtype=torch.bfloat16, device="cuda")
+        call = case.call(c, out)
+        call()
+        torch.cuda.synchronize()
+        assert {(k[0], k[3]) for k in launched(call)} == {(SHAPES[shape], 64 * (shape % 10))}
+        err = np.abs(out.cpu().double().numpy().reshape(case.want.shape) - case.want)
+        say(f"cancelling values, {bits} bits, {shape}: error {err.max() / terms:.1e} of the terms, "
+            f"{np.linalg.norm(err) / np.linalg.norm(case.want):.1e} of the outputs")
+        assert (err <= case.tol[int(shape == 818)]).all()
+
+
 @pytest.mark.parametrize("shape", [0, 418, 818])
 def test_attention_beyond_32_bit_offsets(shape, monkeypatch):
     """The last plane of a packed cache of more than 4 GiB: queries that find the first and the very last position among
