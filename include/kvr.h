@@ -364,7 +364,8 @@ kvr_status kvr_transplant(kvr_ctx *ctx, const void *d_src, int32_t src_n_cap, vo
  * (the order in which the matrix units take them; nibbles and bytes count from the
  * low end).  A packed cache is 16-byte aligned; kvr_packed_bytes() gives its size.
  * It needs no initialisation: what no call wrote has no effect, except on a query row
- * whose position is behind it.
+ * whose position is behind it.  kvr_transplant and the GPU selectors take unpacked
+ * caches (kvr_unpack makes one).
  *
  * In the calls below `bits` other than 4 or 8 is KVR_E_UNSUPPORTED.  A cache does not
  * say its bits or its dimensions: every call on it names those that it was written with,

@@ -13,11 +13,11 @@
 //
 // The pairs are double buffered, one barrier per block of keys; the packed words of
 // the block after the next are in flight meanwhile.  Matrix and vector instructions
-// bound it together: over a prompt of 4000 tokens (32 heads of 8, 4 bits, 285 us) the
+// bound it together: over a prompt of 4000 tokens (32 heads of 8, 4 bits, 290 us) the
 // matrix units are busy half of the time and the vector units 45 %.  Without the
 // staging it would take 227 us, with one output product of three 240, without its LDS
-// reads 258, without exponentials 263.  Operands read further ahead, and staging put
-// between the matrix instructions, changed nothing (290 to 312).  Zero times a value that is not
+// reads 258, without exponentials 263.  Operands read further ahead (313) and staging put
+// between the matrix instructions (up to 312) were slower.  Zero times a value that is not
 // finite is not zero, so such values are staged as zeros and flagged, and the rows
 // that see their slot get NaN afterwards.
 #include "attention_packed.h"

@@ -733,15 +733,17 @@ hipError_t plan_documents(const kvr_ctx *c, int bits, bool pair, const std::vect
         // Little work takes blocks of eight wavefronts, whose partials are fewer (one
         // document of 40001 positions 17.5 us, blocks of four 18.7); much work, six steps for
         // each wavefront of 768 blocks of four, takes those, which come out more even (64
-        // documents 80 and 90).
+        // documents 80 and 90).  768 are what a device holds of the 128-wide kernel with
+        // 4 bits and one piece a query; the others hold 512 to 1024, which the threshold,
+        // measured on that one, does not tell apart.
         sh.copies = most <= 4 ? 4 : most <= 8 ? 2 : 1;
         if (units >= 6ll * 768 * 4 * (sh.copies == 4 ? 2 : 1)) sh.waves = 4;
         return plan_shape(c, bits, pair, size, sh, out);
     }
     // Many columns: two or four tiles of them, or the kernel for many rows (us a call, 32
     // heads of 8, 4 bits: 20 rows of 32 documents of 6000 positions 236, 304, 362; 48 rows
-    // of 8 156, 154, 114; 200 rows of 4 292, 294, 217; prompts of 1500 tokens 79, 73, 102
-    // and of 4000 437, 408, 290).
+    // of 8 156, 154, 114; 200 rows of 4 292, 294, 217; prompts of 1500 tokens 81, 76, 103
+    // and of 4000 428, 400, 290).
     hipError_t err = hipSuccess;
     for (const PackedShape s : {PackedShape{4, 1, 8, false}, PackedShape{2, 1, 8, false}, PACKED_ROWS}) {
         if (s.rows && !c->bf16) continue;

@@ -147,8 +147,8 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedWords<N> t, in
 // packed block is put together (or taken apart) in LDS and moves to and from memory
 // in one contiguous piece; where only some positions are listed, their words and
 // bytes move one by one and the others are not touched.  Bound by memory: 32 layers of 8
-// heads, 5000 positions, 4 bits (839 MB) 155 us packed and 138 us read back, 5.4 and
-// 6.1 TB/s (a large copy 4.9; the packed cache is partly in the last-level cache).  With
+// heads, 5000 positions, 4 bits (839 MB) 159 us packed and 139 us read back, 5.3 and
+// 6.0 TB/s (a large copy 4.9; the packed cache is partly in the last-level cache).  With
 // loads that wait for each other and masks for partial rows it was 192 and 178; by one
 // row a wavefront, straight to memory, the two took 1960 us.
 struct PackedUnit {
