@@ -810,10 +810,11 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
         // listed, unless the lists fill more than one table: runs of four column groups or
         // more are then taken out of them, which costs a fifth more groups at most and saves
         // launches (5000 consecutive rows and a repeated one: one launch, six without).
+        // A pass's lists stand in memory and take no room.
         long long words = 0;
         for (int i = 0; i < n_docs; ++i)
             if (parts == 1 || (size[i].cols > 16) == (p == 0)) words += PK_ENTRY + size[i].cols / G;
-        const int least = words > PK_WORDS ? std::max<int>(PK_ENTRY, (int)((4 * cols + G - 1) / G)) : 0;
+        const int least = !row_table && words > PK_WORDS ? std::max<int>(PK_ENTRY, (int)((4 * cols + G - 1) / G)) : 0;
         TableFill fill(nullptr);
         int used = 0;  // partial slots of the launch
         auto open = [&] {

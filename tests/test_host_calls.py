@@ -111,3 +111,16 @@ def test_shapes_can_be_chosen():
             kernel = "attention_packed_rows_kernel<128, %d, 1>" if shape == "818" else \
                 "attention_packed_kernel<unsigned short, 128, %d, 1, " + shape[1] + ", 64>"
             assert l["name"] == kernel % bits
+
+
+def test_a_repairs_rows_are_one_entry():
+    """A pass has its positions in memory: its lists need no room in the launch's table, however long."""
+    launches = run("""
+    c = context(dims(max_ctx=4000, max_rows=1200))
+    host.host_clear()
+    kvr.kvr_repair_packed(c, [kvr.make_doc(P, 4000, 4000, P, 10, 605, list(range(700, 1510, 2)), None)], 4)
+    result = [l for l in launched() if l["name"].startswith("attention_packed_") and "combine" not in l["name"]]
+    """)
+    # 1000 rows of four heads; 595 and 405 apart were 10 + 7 groups of 256 columns, 38 + 26 of 64, 75 + 51 of 32
+    groups = (16,) if "rows" in launches[0]["name"] else (63, 125)
+    assert len(launches) == 1 and any(launches[0]["grid"][1] % g == 0 for g in groups)
