@@ -25,6 +25,7 @@ def _library() -> str:
 
 PRELUDE = """
 import ctypes, json, sys
+sys.modules["torch"] = None  # (the library is loaded without it, and it would take seconds)
 host = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
 host.host_log.restype = ctypes.c_char_p
 import paper_2609_17983_amd as kvr
