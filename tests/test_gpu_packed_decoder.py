@@ -78,3 +78,23 @@ def test_repair_packed_of_more_documents_than_a_table_holds():
             y = check_pass(p, before[i], packed[i].cpu().numpy(), toks[i].cpu().numpy(), P, n, f"document {i}")
             assert relmax(hidden[i].cpu().numpy(), y) <= TOL[kvr.KVR_BF16], i
         assert len(launched(call)) > MID.n_layers  # more than one launch a layer
+
+
+@pytest.mark.parametrize("model,dtype,bits", [(MID, kvr.KVR_BF16, 4), (synth.TINY, kvr.KVR_F32, 8)])
+def test_score_and_generate_packed_from_nothing(model, dtype, bits):
+    """A cache without a context, more rows than the LM head takes at once, and a continuation by one token."""
+    m = 150
+    with Packed(model, dtype, m + 2, 64, bits) as p:
+        toks = torch.zeros(m + 2, dtype=torch.int32)
+        toks[:m] = synth.make_tokens(m, model.vocab)
+        dev, lp = toks.cuda(), torch.zeros(m, device="cuda")
+        before = p.bytes().copy()
+        kvr.kvr_score_packed(p.ctx, p.cache.data_ptr(), bits, 0, m + 2, dev.data_ptr(), m, lp.data_ptr(), None, stream())
+        after = p.bytes().copy()
+        logits = check_pass(p, before, after, toks.numpy(), range(m), m + 2, "score") @ p.lm.T
+        want = logits - logits.max(-1, keepdims=True)
+        want -= np.log(np.exp(want).sum(-1, keepdims=True))
+        assert relmax(lp[:m - 1].cpu().numpy(), want[np.arange(m - 1), toks.numpy()[1:m]]) <= TOL[dtype]
+        kvr.kvr_generate_packed(p.ctx, p.cache.data_ptr(), bits, 0, m + 2, dev.data_ptr(), 1, 2, stream())
+        end, got = p.bytes(), dev.cpu().numpy()
+        check_pass(p, after, end, got, range(2), m + 2, "generate")

@@ -124,3 +124,21 @@ def test_a_repairs_rows_are_one_entry():
     # 1000 rows of four heads; 595 and 405 apart were 10 + 7 groups of 256 columns, 38 + 26 of 64, 75 + 51 of 32
     groups = (16,) if "rows" in launches[0]["name"] else (63, 125)
     assert len(launches) == 1 and any(launches[0]["grid"][1] % g == 0 for g in groups)
+
+
+def test_profile_counts_the_launches_of_packed_passes():
+    steps, launches = run("""
+    c = context(dims(3, 4, 2, 64, max_ctx=4000))
+    kvr.kvr_profile_enable(c, True)
+    host.host_clear()
+    kvr.kvr_generate_packed(c, P, 4, 3000, 4000, P, 3, 2)
+    counted = kvr.kvr_profile_read(c)
+    made = launched()
+    kvr.kvr_attention_packed(c, 0, 4, kvr.make_packed_rows([(P, 4000, [9])]), P, 256, P, 256)  # no pass, not counted
+    assert kvr.kvr_profile_read(c) == {} or not any(n for _, n in kvr.kvr_profile_read(c).values())
+    result = [{k: n for k, (_, n) in counted.items()}, made]
+    """)
+    names = [l["name"] for l in launches]
+    assert steps["attention"] == sum(n.startswith("attention_packed_kernel") for n in names) == 3 * 2
+    assert steps["attention_combine"] == sum("combine" in n for n in names)
+    assert steps["rope_scatter"] == sum(n.startswith("rope_pack_kernel") for n in names) == 3 * 2
