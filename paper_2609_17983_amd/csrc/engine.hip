@@ -808,8 +808,11 @@ hipError_t plan_packed(const kvr_ctx *c, Tables &t, int bits, bool pair, int n_d
         const long long slots = (long long)(c->attn_part_floats / ((size_t)cols * pk_part_row(c->d.head_dim))) / Hkv;
         // An entry's last column group is part empty, so a document's rows are one entry,
         // listed, unless the lists fill more than one table: runs of four column groups or
-        // more are then taken out of them, which costs a fifth more groups at most and saves
-        // launches (5000 consecutive rows and a repeated one: one launch, six without).
+        // more are then taken out of them, which saves launches and brings up to two part
+        // empty groups each (us a call, before and so: 5000 rows and one more 1217 and 473;
+        // rows of one document with single ones between them, 32 heads, runs of 330 rows
+        // 1333 and 594; 128 heads, runs of 140 rows, 9 groups, 1737 and 1453, of 66 rows,
+        // 5 groups, 1916 and 1970; runs of two groups taken out too, 33 rows, 1906 and 3284).
         // A pass's lists stand in memory and take no room.
         long long words = 0;
         for (int i = 0; i < n_docs; ++i)
