@@ -17,8 +17,8 @@
 // is a sum per group and column, added to the output once, at the end.  fp32 models
 // take the codes less half their range (c - 8, c - 128) and the groups' middles
 // m + 8 s, m + 128 s: the products then have no common part to cancel, which cost
-// two bits (an output's error against 64 bits 1.8e-6; so 0.4e-6 to 0.6e-6, the same
-// attention in plain fp32 0.9e-6).  Nothing is dequantised, and scores and sums are
+// two bits (an output's error against 64 bits 1.8e-6; so 0.3e-6 to 0.6e-6, the same
+// attention in plain fp32 0.4e-6 to 0.9e-6).  Nothing is dequantised, scores and sums are
 // fp32.  Matrix operands that are not codes go in as bf16 pieces, an MFMA each: a bf16
 // query is one, a compensated pair two, an fp32 query three (all 24 bits); p s is two
 // (16 bits, of the largest term: outputs of 2^-11 of their terms are off by 3e-3) with
